@@ -288,6 +288,120 @@ gtp_status gtp_selfproduct(int L, int nu, int Lout, unsigned mode, const void *x
 gtp_status gtp_sh_filter(int L, const float *r, const float *h, int64_t B, int64_t C, float *out,
                          void *stream);
 
+/* ---- The layers around the product -------------------------------------
+ * Normalisation, dropout and attention of a block that holds Gaunt products.
+ * Each commutes with rotations of the SH features: the normalisation scales a
+ * degree as a whole, dropout drops a channel as a whole, and attention takes
+ * dot products of whole heads, which a rotation leaves alone.
+ *
+ * Unlike the products these write results (y, dx, o, dq, dk, dv) in the type of
+ * their inputs, rounded once; statistics and weight gradients are fp32, as is
+ * every sum.  No device memory is allocated: what a call needs beside its
+ * outputs is the caller's `work` (16-byte aligned, at least the bytes that the
+ * _work function of the same arguments names, its contents of no interest
+ * before or after), so every call can be captured in a graph.  No atomics: the
+ * same call gives the same bits.  Data read on one stream and written on
+ * another is the caller's to order. */
+
+/* Normalisation of SH features by degree.  x: [N, C, (L+1)^2] of `dtype`; with
+ *   mu = mean_c x[n, c, 0],  v_l = mean over (c, m) of (x[n, c, (l, m)] - mu [l = 0])^2:
+ *   y[n, c, (l, m)] = (x[n, c, (l, m)] - mu [l = 0]) rstd_l w[l, c] + b[c] [l = 0],
+ *   rstd_l = 1 / sqrt(v_l + eps).
+ * L = 0 is the ordinary layer norm over C channels.  w: [L+1, C] fp32 or NULL
+ * (ones); b: [C] fp32 or NULL (zeros); eps > 0; y: like x, may be x itself, else
+ * not overlapping it; mean: [N] and rstd: [N, L+1] fp32, what the backward
+ * reads, or NULL.  0 <= L <= 64; N C == 0 is a no-op.  GTP_ERR_UNSUPPORTED above
+ * 2^31 - 1 rows or channels. */
+gtp_status gtp_layer_norm(int L, const void *x, gtp_dtype dtype, const float *w, const float *b, float eps, int64_t N,
+                          int64_t C, void *y, float *mean, float *rstd, void *stream);
+
+/* Bytes of `work` of gtp_layer_norm_backward (-1 on a bad argument); needed
+ * only where dw or db is asked for. */
+int64_t gtp_layer_norm_backward_work(int L, gtp_dtype dtype, int64_t N, int64_t C);
+
+/* Gradient of gtp_layer_norm for dy (like x): with xh = (x - mu [l = 0]) rstd_l
+ * and g = dy w,
+ *   dx = rstd_l (g - xh mean_{c,m}(g xh) - [l = 0] mean_c g)   (like x; may be dy itself),
+ *   dw[l, c] = sum_{n,m} dy xh   [L+1, C],   db[c] = sum_n dy[n, c, 0]   [C], fp32.
+ * mean, rstd: as gtp_layer_norm wrote them.  dx, dw, db may each be NULL (not
+ * computed); they are written, not accumulated.  N C == 0 writes zero weight
+ * gradients. */
+gtp_status gtp_layer_norm_backward(int L, const void *x, gtp_dtype dtype, const float *w, const float *mean,
+                                   const float *rstd, const void *dy, int64_t N, int64_t C, void *dx, float *dw,
+                                   float *db, void *work, int64_t work_bytes, void *stream);
+
+/* Dropout of groups of K consecutive elements (all (L+1)^2 coefficients of a
+ * channel, or K = 1) added to a residual:
+ *   y = res + keep x / (1 - p),   keep = 0 with probability p, else 1,
+ * one draw for each of `groups` groups.  The mask is never stored: the draw of
+ * group g is halfword g mod 8 of the 128 bits that Philox4x32-10 (Salmon et al.,
+ * SC 2011) gives for counter (g / 8, rng[1]) and key rng[0], kept where it is at
+ * least round(65536 p) (at most 65535), so p counts in units of 2^-16 and 1 - p
+ * above is that of the unit.  rng: two uint64 in device memory, seed and offset,
+ * read when the call runs: a graph that is replayed draws anew where they were
+ * changed between.  The gradient is the same call on dy, without res.
+ * x, res (or NULL), y: [groups, K] of `dtype`; y may be x or res itself, else not
+ * overlapping them.  0 <= p < 1.  groups K == 0 is a no-op. */
+gtp_status gtp_dropout(const void *x, const void *res, gtp_dtype dtype, double p, const uint64_t *rng, int64_t groups,
+                       int64_t K, void *y, void *stream);
+
+/* Rows of a tensor [rows, heads, d]: element (t, h, i) at data[t row + h head + i]. */
+typedef struct {
+  void *data;
+  int64_t row, head;
+} gtp_rows;
+
+/* What both directions of the attention share.  The rows of B segments (the
+ * atoms of each molecule) lie one after the other: queries of segment b are rows
+ * q_off[b] .. q_off[b+1] - 1 of q, its keys rows k_off[b] .. k_off[b+1] - 1 of k
+ * and v.  Offsets are device arrays [B+1], ascending, read when the call runs;
+ * NULL: equal segments of max_q (max_k) rows.  A segment longer than max_q
+ * (max_k), and an offset outside the tensor, is cut there.  Rows of no segment are
+ * not written. */
+typedef struct {
+  gtp_dtype dtype;          /* of q, k, v, o and the gradients */
+  int H, Hk, d;             /* query heads, key heads (H a multiple of Hk: head h reads key head h / (H / Hk)),
+                               head length 1..256 (c channels of degree L: c (L+1)^2) */
+  int64_t B, Tq, Tk;        /* segments, rows of q, rows of k and v */
+  int64_t max_q, max_k;     /* the longest segment's rows */
+  const int64_t *q_off, *k_off;
+  const uint8_t *key_mask;  /* [Tk]: 0 = absent key, as if its row were not there, whatever it holds; or NULL */
+  float scale;              /* of the scores */
+  double p;                 /* probabilities dropped with probability p, 0 <= p < 1 */
+  const uint64_t *rng;      /* device {seed, offset}; may be NULL where p is 0 */
+} gtp_attn;
+
+/* Bytes of `work` of gtp_attention (backward = 0) or gtp_attention_backward (1);
+ * -1 on a bad argument. */
+int64_t gtp_attention_work(const gtp_attn *a, int backward);
+
+/* Softmax attention over each segment:
+ *   s = scale q k^T,  P = softmax(s) over the segment's present keys,
+ *   o = (m P) v,  lse = log sum_j exp(s_j),
+ * m the factors 0 or 1 / (1 - p) of dropped probabilities.  A row without a
+ * present key (or whose every score is -infinity) has o = 0 and lse = -infinity.
+ * q, o: [Tq, H, d]; k, v: [Tk, Hk, d]; lse: [Tq, H] fp32.  Any nonnegative strides
+ * for inputs; outputs' rows must not overlap each other or an input.  The draws,
+ * of the generator of gtp_dropout: the rows of a key head's G = H / Hk query heads
+ * count together, R = i G + g for row i of the segment, in blocks of 4 rows x 4
+ * keys; block ((b Hk + hk) ceil(max_q G / 4) + R / 4) ceil(max_k / 4) + j / 4 takes
+ * calls 2 block (its first two rows) and 2 block + 1, element (R, j) halfword
+ * 4 (R mod 2) + j mod 4.  Sums are fp32; with bf16 inputs P and (in the backward)
+ * the scores' gradients enter the matrix products rounded to bf16. */
+gtp_status gtp_attention(const gtp_attn *a, const gtp_rows *q, const gtp_rows *k, const gtp_rows *v, const gtp_rows *o,
+                         float *lse, void *work, int64_t work_bytes, void *stream);
+
+/* Gradient of gtp_attention for dout: the probabilities are made again from lse
+ * and the draws from the generator, nothing of size rows x keys is stored:
+ *   P = exp(s - lse),  dS = P (m (dout v^T) - delta),  delta = sum_i dout_i o_i,
+ *   dq = scale dS k,  dk = scale dS^T q,  dv = (m P)^T dout,
+ * dk and dv summed over the query heads of a key head.  o, lse: as gtp_attention
+ * wrote them.  dq, or dk and dv, may be NULL (not computed).  Absent keys have
+ * zero gradients.  GTP_ERR_INVALID_ARG where only one of dk and dv is NULL. */
+gtp_status gtp_attention_backward(const gtp_attn *a, const gtp_rows *q, const gtp_rows *k, const gtp_rows *v,
+                                  const gtp_rows *o, const gtp_rows *dout, const float *lse, const gtp_rows *dq,
+                                  const gtp_rows *dk, const gtp_rows *dv, void *work, int64_t work_bytes, void *stream);
+
 /* HBM streaming probe (measurement aid: the roof the HBM-bound kernels are
  * read against; each workgroup streams one contiguous chunk, the chunks
  * dealt to the XCDs in contiguous runs).  mode 0: read nbytes of src (dst: a

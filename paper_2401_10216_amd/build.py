@@ -22,7 +22,9 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libgtp.so")
 
 HIP_SOURCES = ["gtp_api.hip", "gtp_small.hip", "gtp_wave.hip", "gtp_mfma.hip", "gtp_generic.hip", "gtp_escn.hip",
-               "gtp_escn_wave.hip", "gtp_mix.hip", "gtp_mixq.hip", "gtp_probe.hip", "gtp_wgrad.hip", "gtp_wbwd.hip"]
+               "gtp_escn_wave.hip", "gtp_mix.hip", "gtp_mixq.hip", "gtp_probe.hip", "gtp_wgrad.hip", "gtp_wbwd.hip",
+               "gtp_layers.hip", "gtp_norm.hip", "gtp_drop.hip", "gtp_attn_fwd.hip", "gtp_attn_dq.hip",
+               "gtp_attn_dkv.hip"]
 CPP_SOURCES = ["gtp_tables.cpp", "gtp_escn_tables.cpp", "gtp_mfma_tables.cpp"]
 ARCH = "gfx950"
 # Packed fp32 VALU forms stay off: plain fp32 FMAs only.

@@ -19,6 +19,7 @@
 #include "../../include/gtp.h"
 #include "gtp_device.hpp"
 #include "gtp_escn.hpp"
+#include "gtp_layers.hpp"
 #include "gtp_mfma_tables.hpp"
 #include "gtp_mixq.hpp"
 #include "gtp_mixq_tables.hpp"
@@ -467,6 +468,16 @@ gtp_status escn_wave16_run(gtp_plan p, const void* x, int it, const float* r, co
 }
 
 }  // namespace
+
+// The message of entries in other files.
+gtp_status gtp::set_error(gtp_status s, const char* msg) noexcept {
+  try {
+    g_last_error = msg;
+  } catch (...) {
+    g_last_error.clear();
+  }
+  return s;
+}
 
 extern "C" {
 

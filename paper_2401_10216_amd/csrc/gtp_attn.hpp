@@ -1,0 +1,43 @@
+// Softmax attention over packed segments and its gradient: what the C entries
+// (gtp_layers.hip) hand to the kernels (gtp_attn_fwd.hip, gtp_attn_dq.hip,
+// gtp_attn_dkv.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace gtp {
+
+// Rows of a tensor [rows, heads, d]: element (t, h, i) at p[t row + h head + i].
+struct AttnRows {
+  const void* p;
+  int64_t row, head;
+};
+
+struct AttnArgs {
+  AttnRows q, k, v, o, dout;  // inputs (o and dout in the backward)
+  AttnRows out;               // o of the forward, dq of the backward (p = null: not asked for)
+  AttnRows dk, dv;            // null: not asked for
+  const int64_t *q_off, *k_off;  // [B + 1] or null: equal segments of max_q, max_k rows
+  const uint8_t* mask;           // [Tk] or null
+  float* lse;                    // [Tq, H]: written by the forward, read by the backward
+  float* delta;                  // [Tq, H]: rows' sums of dout o
+  float* part;                   // partial results of split calls
+  const uint64_t* rng;           // {seed, offset}, with threshold > 0
+  int64_t B, Tq, Tk, max_q, max_k;
+  int H, Hk, G, d;               // query heads, key heads, H / Hk, head length
+  int splits;                    // parts that a row's keys (or a key's rows) are dealt to
+  float scale, scale2;           // of the scores; times log2(e)
+  uint32_t threshold;            // 0: nothing is dropped
+  float keep;                    // factor of what is kept
+  bool bf16, vec;                // vec: every row of every tensor starts 16-byte aligned, d a multiple of 16 bytes
+};
+
+int attn_padded(int d);  // the head length that the kernels are instantiated at, >= d
+hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_delta(const AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_dq(const AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_dkv(const AttnArgs& a, hipStream_t s);
+
+}  // namespace gtp

@@ -1,0 +1,276 @@
+// What the attention kernels share: the matrix products on a wave's 32 x 32
+// tile, the staging of row tiles in LDS, segments, and dropped probabilities.
+//
+// A wave takes 32 columns (query rows in the forward and in dq, keys in dk and
+// dv) as the N index of every product, and walks the other axis in tiles of 32
+// as the M index.  The 32 x 32 result of a product lies with column lane & 31
+// in a lane, rows 8 (r / 4) + 4 (lane >> 5) + r % 4 in its registers r < 16: that
+// is, up to the order of the summed index, the layout in which the next product
+// takes its N-side operand.  So probabilities go from accumulator to operand
+// without crossing lanes, a column's statistics live in one lane (and its
+// partner, lane ^ 32), and the M-side operand follows the same order.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "gtp_attn.hpp"
+#include "gtp_device.hpp"
+#include "gtp_rng.hpp"
+
+namespace gtp {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Row r of a wave's 32 x 32 result in register r (0..15) of lane half hi.
+__device__ __forceinline__ constexpr int tile_row(int r, int hi) { return 8 * (r >> 2) + 4 * hi + (r & 3); }
+
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+  return z;
+}
+
+// acc += A B over the 32 bytes of the summed axis (8 fp32 or 16 bf16 values)
+// of which the lane holds its half's 16: A's of row lane & 31, B's of column
+// lane & 31.
+template <typename T>
+__device__ __forceinline__ void mma_chunk(const u32x4& a, const u32x4& b, f32x16& acc) {
+  if constexpr (sizeof(T) == 4) {
+    const f32x4 fa = __builtin_bit_cast(f32x4, a), fb = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[i], fb[i], acc, 0, 0, 0);
+  } else {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0,
+                                                  0, 0);
+  }
+}
+
+// A row tile in LDS: rows of DP elements, 16 bytes of padding behind each (the
+// lanes of a product's operand read take the same columns of 32 rows: an odd
+// stride in units of 16 bytes spreads them over the banks).
+template <typename T, int DP>
+constexpr int tile_stride() {
+  return DP * int(sizeof(T)) + 16;
+}
+
+// The operand of columns 32 c .. 32 c + 31 (bytes) of row `row` of a tile.
+template <typename T, int DP>
+__device__ __forceinline__ u32x4 tile_chunk(const char* tile, int row, int c, int hi) {
+  return *reinterpret_cast<const u32x4*>(tile + row * tile_stride<T, DP>() + 32 * c + 16 * hi);
+}
+
+// acc[d, column] += sum over the 32 rows of a tile of tile[row][32 dt + d] p[row, column],
+// p in the layout of a result (fp32; rounded to the tile's type where that is
+// bf16: half a unit in 2^-8 of each probability or score gradient, as the
+// operands' own rounding).
+template <typename T, int DP>
+__device__ __forceinline__ void mma_transposed(const char* tile, int dt, const f32x16& p, int lane, f32x16& acc) {
+  constexpr int S = tile_stride<T, DP>();
+  const int hi = lane >> 5;
+  if constexpr (sizeof(T) == 4) {
+    const char* base = tile + 4 * hi * S + (32 * dt + (lane & 31)) * 4;
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(base + tile_row(r, 0) * S), p[r], acc,
+                                                 0, 0, 0);
+  } else {
+    // 16 lanes read a block of 4 rows x 16 columns, 8 bytes each, and each
+    // receives the 4 rows of its own column
+    const char* base = tile + (4 * hi + ((lane & 15) >> 2)) * S + (32 * dt + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+    typedef __attribute__((address_space(3))) s16x4* lds4;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(base + 16 * s * S));
+      const s16x4 up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(base + (16 * s + 8) * S));
+      bf16x8 a, b;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        a[i] = __builtin_bit_cast(__bf16, short(lo[i]));
+        a[4 + i] = __builtin_bit_cast(__bf16, short(up[i]));
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) b[i] = static_cast<__bf16>(p[8 * s + i]);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
+    }
+  }
+}
+
+// 16 bytes at column `col` (in units of 16 bytes) of a row of d elements;
+// null row: zeros.
+template <typename T>
+__device__ __forceinline__ u32x4 load16(const T* row, int col, int d, bool vec) {
+  u32x4 z = {0u, 0u, 0u, 0u};
+  constexpr int E = 16 / int(sizeof(T));
+  if (row == nullptr || col * E >= d) return z;
+  if (vec) return *reinterpret_cast<const u32x4*>(row + col * E);
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (col * 4 + i < d) z[i] = __float_as_uint(row[col * 4 + i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (col * 8 + i < d) z[i >> 1] |= uint32_t(row[col * 8 + i]) << (16 * (i & 1));
+  }
+  return z;
+}
+
+// ROWS rows from memory to an LDS tile by NT threads: fetch() issues the loads,
+// commit() writes what came.  row(r): pointer to tile row r, null where there is none.
+template <typename T, int DP, int ROWS, int NT>
+struct Stage {
+  static constexpr int CPR = DP * int(sizeof(T)) / 16;
+  static constexpr int ITER = (ROWS * CPR + NT - 1) / NT;
+  u32x4 reg[ITER];
+  template <typename F>
+  __device__ __forceinline__ void fetch(F row, int d, bool vec) {
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+      const int id = int(threadIdx.x) + i * NT;
+      if (ROWS * CPR % NT != 0 && id >= ROWS * CPR) break;
+      reg[i] = load16<T>(row(id / CPR), id % CPR, d, vec);
+    }
+  }
+  __device__ __forceinline__ void commit(char* tile) const {
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+      const int id = int(threadIdx.x) + i * NT;
+      if (ROWS * CPR % NT != 0 && id >= ROWS * CPR) break;
+      *reinterpret_cast<u32x4*>(tile + (id / CPR) * tile_stride<T, DP>() + 16 * (id % CPR)) = reg[i];
+    }
+  }
+};
+
+// Rows [start, start + n) of segment b among `total`, at most `most`; offsets
+// outside the tensor are cut to it, so that no access leaves it.
+__device__ __forceinline__ void segment(const int64_t* off, int64_t b, int64_t most, int64_t total, int64_t& start,
+                                        int64_t& n) {
+  int64_t s = off ? off[b] : b * most, e = off ? off[b + 1] : s + most;
+  s = s < 0 ? 0 : (s > total ? total : s);
+  e = e < s ? s : (e > total ? total : e);
+  start = s;
+  n = e - s < most ? e - s : most;
+}
+
+// Element type of the tensors in memory.
+template <typename T>
+__device__ __forceinline__ float to_f32(T v) {
+  if constexpr (sizeof(T) == 4)
+    return v;
+  else
+    return __uint_as_float(uint32_t(v) << 16);
+}
+
+// d elements of one row from the results acc[dt] (column lane & 31 = the row,
+// results' rows = the elements), times f.
+template <typename T, int NDT>
+__device__ __forceinline__ void store_columns(T* row, const f32x16 (&acc)[NDT], float f, int d0, int d, int hi,
+                                              bool vec) {
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int e = d0 + 32 * dt + 8 * g + 4 * hi;
+      if (e >= d) continue;
+      if constexpr (sizeof(T) == 4) {
+        const f32x4 o = {acc[dt][4 * g] * f, acc[dt][4 * g + 1] * f, acc[dt][4 * g + 2] * f, acc[dt][4 * g + 3] * f};
+        if (vec)
+          *reinterpret_cast<f32x4*>(row + e) = o;
+        else
+          for (int i = 0; i < 4; ++i)
+            if (e + i < d) row[e + i] = o[i];
+      } else {
+        bf16x4 o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = static_cast<__bf16>(acc[dt][4 * g + i] * f);
+        if (vec)
+          *reinterpret_cast<bf16x4*>(row + e) = o;
+        else
+          for (int i = 0; i < 4; ++i) {
+            const __bf16 one = o[i];
+            if (e + i < d) row[e + i] = __builtin_bit_cast(uint16_t, one);
+          }
+      }
+    }
+}
+
+// Dropped probabilities.  The rows of a key head's G query heads count together
+// (row R = i G + g of the segment), in blocks of 4 rows x 4 keys: block
+// ((b Hk + hk) ceil(max_q G / 4) + R / 4) ceil(max_k / 4) + j / 4 takes calls 2 block
+// (rows 0, 1) and 2 block + 1 (rows 2, 3) of the generator, element (R, j) halfword
+// 4 (R % 2) + j % 4.
+struct Drop {
+  uint64_t seed, offset, base, nc;
+  uint32_t threshold;
+  __device__ __forceinline__ void init(const AttnArgs& a, int64_t b, int hk) {
+    seed = a.rng[0];
+    offset = a.rng[1];
+    threshold = a.threshold;
+    nc = uint64_t(a.max_k + 3) >> 2;
+    const uint64_t nr = uint64_t(a.max_q * a.G + 3) >> 2;
+    base = (uint64_t(b) * a.Hk + hk) * nr * nc;
+  }
+  // Bit r of the result: whether element (row R, key j0 + tile_row(r, hi)) is kept.
+  __device__ __forceinline__ uint32_t keys_of_row(int64_t R, int64_t j0, int hi) const {
+    uint32_t keep = 0;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const uint64_t block = base + uint64_t(R >> 2) * nc + uint64_t((j0 + 8 * g + 4 * hi) >> 2);
+      uint32_t w[4];
+      philox(2 * block + ((R >> 1) & 1), seed, offset, w);
+      const uint32_t a = (R & 1) ? w[2] : w[0], b = (R & 1) ? w[3] : w[1];
+      keep |= ((a & 0xffffu) >= threshold ? 1u : 0u) << (4 * g);
+      keep |= ((a >> 16) >= threshold ? 1u : 0u) << (4 * g + 1);
+      keep |= ((b & 0xffffu) >= threshold ? 1u : 0u) << (4 * g + 2);
+      keep |= ((b >> 16) >= threshold ? 1u : 0u) << (4 * g + 3);
+    }
+    return keep;
+  }
+  // Bit r: whether element (row R0 + tile_row(r, hi), key j) is kept.
+  __device__ __forceinline__ uint32_t rows_of_key(int64_t j, int64_t R0, int hi) const {
+    uint32_t keep = 0;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const uint64_t block = base + uint64_t((R0 + 8 * g + 4 * hi) >> 2) * nc + uint64_t(j >> 2);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t w[4];
+        philox(2 * block + h, seed, offset, w);
+        const uint32_t a = (j & 2) ? w[1] : w[0], b = (j & 2) ? w[3] : w[2];
+        const int sh = 16 * int(j & 1);
+        keep |= (((a >> sh) & 0xffffu) >= threshold ? 1u : 0u) << (4 * g + 2 * h);
+        keep |= (((b >> sh) & 0xffffu) >= threshold ? 1u : 0u) << (4 * g + 2 * h + 1);
+      }
+    }
+    return keep;
+  }
+};
+
+// Work of a workgroup: tiles fastest, then splits, key heads, segments; XCD-aware,
+// so that the workgroups that read one segment's rows share an L2.
+struct Work {
+  int tile, split, hk;
+  int64_t b;
+  __device__ __forceinline__ Work(int64_t w, int64_t n, int tiles, int splits, int Hk) {
+    int64_t id = xcd_product(w, n);
+    tile = int(id % tiles);
+    id /= tiles;
+    split = int(id % splits);
+    id /= splits;
+    hk = int(id % Hk);
+    b = id / Hk;
+  }
+};
+
+}  // namespace gtp

@@ -1,0 +1,152 @@
+// Softmax attention, gradients of the keys and values: with P, dP, dS as for
+// dq (gtp_attn_dq.hip),
+//   dv = (P m)^T dout,  dk = scale dS^T q,
+// summed over the rows of every query head that shares the key head, in order.
+#include "gtp_attn_core.hpp"
+
+namespace gtp {
+namespace {
+
+constexpr int NW = 4, NT = 64 * NW, BK = 32 * NW;
+
+// Workgroup: 128 keys of one key head (4 waves x 32), rows in tiles of 32.  Heads
+// longer than 128 are dealt to `parts` workgroups by output elements (DO each):
+// the accumulators of all of them would not fit the registers.
+template <typename T, int DP, int DO, bool DROP>
+__global__ __launch_bounds__(NT) void k_attn_dkv(const AttnArgs a, int64_t n_wg, int tiles) {
+  constexpr int BR = 32, NC = DP * int(sizeof(T)) / 32, NDT = DO / 32, PARTS = DP / DO;
+  __shared__ __align__(16) char tq[BR * tile_stride<T, DP>()];
+  __shared__ __align__(16) char tg[BR * tile_stride<T, DP>()];
+  __shared__ __align__(16) float t_ref[BR], t_delta[BR];
+  lds_poison(reinterpret_cast<float*>(tq), int(sizeof(tq) / 4));
+  lds_poison(reinterpret_cast<float*>(tg), int(sizeof(tg) / 4));
+  lds_poison(t_ref, BR);
+  lds_poison(t_delta, BR);
+  const Work w(blockIdx.x, n_wg, tiles * PARTS, a.splits, a.Hk);
+  const int tile = w.tile / PARTS, part = w.tile % PARTS;
+  int64_t qs, nq, ks, nk;
+  segment(a.q_off, w.b, a.max_q, a.Tq, qs, nq);
+  segment(a.k_off, w.b, a.max_k, a.Tk, ks, nk);
+  if (int64_t(tile) * BK >= nk) return;
+  const int64_t rows = nq * a.G;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l31 = lane & 31, hi = lane >> 5;
+  const int64_t j = int64_t(tile) * BK + wave * 32 + l31;
+  const bool there = j < nk;
+  const bool present = there && (!a.mask || a.mask[ks + j]);  // an absent key's row is not read; its gradients are zero
+  u32x4 kf[NC], vf[NC];
+  {
+    const T* k = present ? static_cast<const T*>(a.k.p) + (ks + j) * a.k.row + w.hk * a.k.head : nullptr;
+    const T* v = present ? static_cast<const T*>(a.v.p) + (ks + j) * a.v.row + w.hk * a.v.head : nullptr;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      kf[c] = load16<T>(k, 2 * c + hi, a.d, a.vec);
+      vf[c] = load16<T>(v, 2 * c + hi, a.d, a.vec);
+    }
+  }
+  f32x16 ak[NDT], av[NDT];
+#pragma unroll
+  for (int i = 0; i < NDT; ++i) ak[i] = zero16(), av[i] = zero16();
+  Drop drop;
+  if constexpr (DROP) drop.init(a, w.b, w.hk);
+
+  const int64_t ntile = (rows + BR - 1) / BR, per = (ntile + a.splits - 1) / a.splits;
+  const int64_t r_end = (w.split + 1) * per * BR < rows ? (w.split + 1) * per * BR : rows;
+  Stage<T, DP, BR, NT> sq, sg;
+  for (int64_t r0 = w.split * per * BR; r0 < r_end; r0 += BR) {
+    auto row = [&](const AttnRows& t, int r) -> const T* {
+      const int64_t R = r0 + r;
+      return R < rows ? static_cast<const T*>(t.p) + (qs + R / a.G) * t.row + (w.hk * a.G + R % a.G) * t.head : nullptr;
+    };
+    sq.fetch([&](int r) { return row(a.q, r); }, a.d, a.vec);
+    sg.fetch([&](int r) { return row(a.dout, r); }, a.d, a.vec);
+    float ref = INFINITY, delta = 0.0f;
+    if (threadIdx.x < BR && r0 + threadIdx.x < rows) {
+      const int64_t R = r0 + threadIdx.x, at = (qs + R / a.G) * a.H + w.hk * a.G + R % a.G;
+      const float lse = a.lse[at];
+      ref = lse == -INFINITY ? INFINITY : lse * kLog2e;
+      delta = a.delta[at];
+    }
+    __syncthreads();
+    sq.commit(tq);
+    sg.commit(tg);
+    if (threadIdx.x < BR) {
+      t_ref[threadIdx.x] = ref;
+      t_delta[threadIdx.x] = delta;
+    }
+    __syncthreads();
+    f32x16 s = zero16(), dp = zero16();
+#pragma unroll
+    for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tq, l31, c, hi), kf[c], s);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tg, l31, c, hi), vf[c], dp);
+    uint32_t keep = 0xffffu;
+    if constexpr (DROP) keep = drop.rows_of_key(j, r0, hi);
+    f32x16 p;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 rf = *reinterpret_cast<const f32x4*>(t_ref + 8 * g + 4 * hi);
+      const f32x4 de = *reinterpret_cast<const f32x4*>(t_delta + 8 * g + 4 * hi);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 4 * g + i;
+        const float e = exp2f(fmaf(s[r], a.scale2, -rf[i]));
+        if constexpr (DROP) {
+          const bool kept = (keep >> r) & 1u;
+          p[r] = kept ? e : 0.0f;
+          s[r] = e * ((kept ? dp[r] * a.keep : 0.0f) - de[i]);
+        } else {
+          p[r] = e;
+          s[r] = e * (dp[r] - de[i]);
+        }
+      }
+    }
+    // rows past the end and rows without a key count nothing, whatever k and v
+    // hold (a zero of theirs times an infinity would be NaN)
+    if (__any(t_ref[l31] == INFINITY)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (t_ref[tile_row(r, 0) + 4 * hi] == INFINITY) p[r] = s[r] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < NDT; ++i) {
+      mma_transposed<T, DP>(tg, part * NDT + i, p, lane, av[i]);
+      mma_transposed<T, DP>(tq, part * NDT + i, s, lane, ak[i]);
+    }
+  }
+  if (!there) return;
+  if (!present)
+#pragma unroll
+    for (int i = 0; i < NDT; ++i) ak[i] = zero16(), av[i] = zero16();
+  if (a.dk.p)
+    store_columns<T>(static_cast<T*>(const_cast<void*>(a.dk.p)) + (ks + j) * a.dk.row + w.hk * a.dk.head, ak, a.scale,
+                     part * DO, a.d, hi, a.vec);
+  if (a.dv.p)
+    store_columns<T>(static_cast<T*>(const_cast<void*>(a.dv.p)) + (ks + j) * a.dv.row + w.hk * a.dv.head, av,
+                     DROP ? a.keep : 1.0f, part * DO, a.d, hi, a.vec);
+}
+
+template <typename T, int DP>
+hipError_t launch(const AttnArgs& a, hipStream_t s) {
+  constexpr int DO = DP > 128 ? DP / 2 : DP;
+  const int64_t tiles = (a.max_k + BK - 1) / BK, n = tiles * (DP / DO) * a.splits * a.Hk * a.B;
+  if (a.threshold)
+    k_attn_dkv<T, DP, DO, true><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
+  else
+    k_attn_dkv<T, DP, DO, false><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_dkv(const AttnArgs& a, hipStream_t s) {
+  switch (attn_padded(a.d)) {
+    case 32: return a.bf16 ? launch<uint16_t, 32>(a, s) : launch<float, 32>(a, s);
+    case 64: return a.bf16 ? launch<uint16_t, 64>(a, s) : launch<float, 64>(a, s);
+    case 96: return a.bf16 ? launch<uint16_t, 96>(a, s) : launch<float, 96>(a, s);
+    case 128: return a.bf16 ? launch<uint16_t, 128>(a, s) : launch<float, 128>(a, s);
+    case 192: return a.bf16 ? launch<uint16_t, 192>(a, s) : launch<float, 192>(a, s);
+    default: return a.bf16 ? launch<uint16_t, 256>(a, s) : launch<float, 256>(a, s);
+  }
+}
+
+}  // namespace gtp

@@ -1,0 +1,137 @@
+// Softmax attention, gradient of the queries: the probabilities are made again
+// from the scores and the rows' lse,
+//   P = exp(scale q k^T - lse),  dP = (dout v^T) m,  dS = P (dP - delta),
+//   dq = scale dS k,  delta = rows' sums of dout o,
+// m the factors 0 or 1 / (1 - p) of dropped probabilities.
+#include "gtp_attn_core.hpp"
+
+namespace gtp {
+namespace {
+
+constexpr int NW = 4, NT = 64 * NW, BM = 32 * NW;
+
+// delta[t, h] = sum_i dout[t, h, i] o[t, h, i]: 16 lanes a row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_delta(const AttnArgs a) {
+  const int64_t n = a.Tq * a.H, id = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4);
+  const int i0 = threadIdx.x & 15;
+  float s = 0.0f;
+  if (id < n) {
+    const int64_t t = id / a.H, h = id % a.H;
+    const T* o = static_cast<const T*>(a.o.p) + t * a.o.row + h * a.o.head;
+    const T* g = static_cast<const T*>(a.dout.p) + t * a.dout.row + h * a.dout.head;
+    for (int i = i0; i < a.d; i += 16) s = fmaf(to_f32<T>(o[i]), to_f32<T>(g[i]), s);
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  if (id < n && i0 == 0) a.delta[id] = s;
+}
+
+// Workgroup: 128 rows of one key head (4 waves x 32), keys in tiles of 32.
+template <typename T, int DP, bool DROP>
+__global__ __launch_bounds__(NT) void k_attn_dq(const AttnArgs a, int64_t n_wg, int tiles) {
+  constexpr int BN = 32, NC = DP * int(sizeof(T)) / 32, NDT = DP / 32;
+  __shared__ __align__(16) char tk[BN * tile_stride<T, DP>()];
+  __shared__ __align__(16) char tv[BN * tile_stride<T, DP>()];
+  lds_poison(reinterpret_cast<float*>(tk), int(sizeof(tk) / 4));
+  lds_poison(reinterpret_cast<float*>(tv), int(sizeof(tv) / 4));
+  const Work w(blockIdx.x, n_wg, tiles, a.splits, a.Hk);
+  int64_t qs, nq, ks, nk;
+  segment(a.q_off, w.b, a.max_q, a.Tq, qs, nq);
+  segment(a.k_off, w.b, a.max_k, a.Tk, ks, nk);
+  const int64_t rows = nq * a.G;
+  if (int64_t(w.tile) * BM >= rows) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l31 = lane & 31, hi = lane >> 5;
+  const int64_t R = int64_t(w.tile) * BM + wave * 32 + l31;
+  const bool there = R < rows;
+  const int64_t qi = there ? qs + R / a.G : 0;
+  const int h = w.hk * a.G + (there ? int(R % a.G) : 0);
+  u32x4 qf[NC], gf[NC];
+  {
+    const T* q = there ? static_cast<const T*>(a.q.p) + qi * a.q.row + h * a.q.head : nullptr;
+    const T* g = there ? static_cast<const T*>(a.dout.p) + qi * a.dout.row + h * a.dout.head : nullptr;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      qf[c] = load16<T>(q, 2 * c + hi, a.d, a.vec);
+      gf[c] = load16<T>(g, 2 * c + hi, a.d, a.vec);
+    }
+  }
+  // rows without a key, and rows past the end: every exponential is zero
+  const float lse = there ? a.lse[qi * a.H + h] : -INFINITY;
+  const float ref = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  const float delta = there ? a.delta[qi * a.H + h] : 0.0f;
+  f32x16 acc[NDT];
+#pragma unroll
+  for (int i = 0; i < NDT; ++i) acc[i] = zero16();
+  Drop drop;
+  if constexpr (DROP) drop.init(a, w.b, w.hk);
+
+  const T* const kb = static_cast<const T*>(a.k.p) + ks * a.k.row + w.hk * a.k.head;
+  const T* const vb = static_cast<const T*>(a.v.p) + ks * a.v.row + w.hk * a.v.head;
+  const uint8_t* const mask = a.mask ? a.mask + ks : nullptr;
+  const int64_t ntile = (nk + BN - 1) / BN, per = (ntile + a.splits - 1) / a.splits;
+  const int64_t j_end = (w.split + 1) * per * BN < nk ? (w.split + 1) * per * BN : nk;
+  Stage<T, DP, BN, NT> sk, sv;
+  for (int64_t j0 = w.split * per * BN; j0 < j_end; j0 += BN) {
+    auto present = [&](int r) { return j0 + r < nk && (!mask || mask[j0 + r]); };
+    sk.fetch([&](int r) { return present(r) ? kb + (j0 + r) * a.k.row : nullptr; }, a.d, a.vec);
+    sv.fetch([&](int r) { return present(r) ? vb + (j0 + r) * a.v.row : nullptr; }, a.d, a.vec);
+    __syncthreads();
+    sk.commit(tk);
+    sv.commit(tv);
+    __syncthreads();
+    f32x16 s = zero16(), dp = zero16();
+#pragma unroll
+    for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tk, l31, c, hi), qf[c], s);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tv, l31, c, hi), gf[c], dp);
+    const uint32_t ok = uint32_t(__ballot(present(l31))) >> (4 * hi);
+    uint32_t keep = 0xffffu;
+    if constexpr (DROP) keep = drop.keys_of_row(R, j0, hi);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float p = exp2f(fmaf(s[r], a.scale2, -ref));
+      const float g = DROP ? ((keep >> r) & 1u ? dp[r] * a.keep : 0.0f) : dp[r];
+      s[r] = (ok >> tile_row(r, 0)) & 1u ? p * (g - delta) : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < NDT; ++i) mma_transposed<T, DP>(tk, i, s, lane, acc[i]);
+  }
+  if (!there) return;
+  store_columns<T>(static_cast<T*>(const_cast<void*>(a.out.p)) + qi * a.out.row + h * a.out.head, acc, a.scale, 0, a.d,
+                   hi, a.vec);
+}
+
+template <typename T, int DP>
+hipError_t launch(const AttnArgs& a, hipStream_t s) {
+  const int64_t tiles = (a.max_q * a.G + BM - 1) / BM, n = tiles * a.splits * a.Hk * a.B;
+  if (a.threshold)
+    k_attn_dq<T, DP, true><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
+  else
+    k_attn_dq<T, DP, false><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_delta(const AttnArgs& a, hipStream_t s) {
+  const uint32_t n = uint32_t((a.Tq * a.H + 15) / 16);
+  if (a.bf16)
+    k_attn_delta<uint16_t><<<n, 256, 0, s>>>(a);
+  else
+    k_attn_delta<float><<<n, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_attn_dq(const AttnArgs& a, hipStream_t s) {
+  switch (attn_padded(a.d)) {
+    case 32: return a.bf16 ? launch<uint16_t, 32>(a, s) : launch<float, 32>(a, s);
+    case 64: return a.bf16 ? launch<uint16_t, 64>(a, s) : launch<float, 64>(a, s);
+    case 96: return a.bf16 ? launch<uint16_t, 96>(a, s) : launch<float, 96>(a, s);
+    case 128: return a.bf16 ? launch<uint16_t, 128>(a, s) : launch<float, 128>(a, s);
+    case 192: return a.bf16 ? launch<uint16_t, 192>(a, s) : launch<float, 192>(a, s);
+    default: return a.bf16 ? launch<uint16_t, 256>(a, s) : launch<float, 256>(a, s);
+  }
+}
+
+}  // namespace gtp

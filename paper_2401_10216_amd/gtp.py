@@ -40,6 +40,19 @@ _I = ctypes.c_int
 _U = ctypes.c_uint
 _DP = ctypes.POINTER(ctypes.c_double)
 
+
+class _Rows(ctypes.Structure):
+    """gtp_rows."""
+    _fields_ = [("data", _P), ("row", _I64), ("head", _I64)]
+
+
+class _Attn(ctypes.Structure):
+    """gtp_attn."""
+    _fields_ = [("dtype", _I), ("H", _I), ("Hk", _I), ("d", _I), ("B", _I64), ("Tq", _I64), ("Tk", _I64),
+                ("max_q", _I64), ("max_k", _I64), ("q_off", _P), ("k_off", _P), ("key_mask", _P),
+                ("scale", ctypes.c_float), ("p", ctypes.c_double), ("rng", _P)]
+
+
 _SIGS = {
     "gtp_plan_create": (_I, [ctypes.POINTER(_P), _I, _I, _I, _U]),
     "gtp_plan_destroy": (_I, [_P]),
@@ -55,6 +68,13 @@ _SIGS = {
     "gtp_fourier2sh": (_I, [_P, _P, _I64, _P, _P]),
     "gtp_selfproduct": (_I, [_I, _I, _I, _U, _P, _I, _I64, _I64, _P, _P]),
     "gtp_sh_filter": (_I, [_I, _P, _P, _I64, _I64, _P, _P]),
+    "gtp_layer_norm": (_I, [_I, _P, _I, _P, _P, ctypes.c_float, _I64, _I64, _P, _P, _P, _P]),
+    "gtp_layer_norm_backward_work": (_I64, [_I, _I, _I64, _I64]),
+    "gtp_layer_norm_backward": (_I, [_I, _P, _I, _P, _P, _P, _P, _I64, _I64, _P, _P, _P, _P, _I64, _P]),
+    "gtp_dropout": (_I, [_P, _P, _I, ctypes.c_double, _P, _I64, _I64, _P, _P]),
+    "gtp_attention_work": (_I64, [_P, _I]),
+    "gtp_attention": (_I, [_P, _P, _P, _P, _P, _P, _P, _I64, _P]),
+    "gtp_attention_backward": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _P]),
     "gtp_stream_probe": (_I, [_I, _P, _P, _I64, _P]),
     "gtp_compute_probe": (_I, [_I, _I64, _P, _DP, _P]),
     "gtp_grid_floats": (_I64, [_P, _I]),
@@ -461,6 +481,227 @@ def gtp_sh_filter(L: int, r, h=None, out=None, stream=None):
     _on_gpu(r, "r")
     _check(lib().gtp_sh_filter(L, pr, hp, B, C, po, _stream(stream)))
     return out
+
+
+class _on_stream:
+    """Allocations for a launch on `stream`: memory that the allocator hands out for a stream is free of that
+    stream's earlier work only, so what a call on another stream than the current one writes is allocated for it."""
+
+    def __init__(self, stream):
+        import torch
+        self.ctx = torch.cuda.stream(stream) if stream is not None else None
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+
+    def __exit__(self, *exc):
+        return self.ctx.__exit__(*exc) if self.ctx is not None else False
+
+
+def _null():
+    return ctypes.c_void_p(None)
+
+
+def _opt(t, name, shape, dtypes, device):
+    return _null() if t is None else _want(t, name, shape, dtypes, device)
+
+
+def _rng_state(rng, device):
+    import torch
+    return _want(rng, "rng", (2,), (torch.int64, torch.uint64), device)
+
+
+def _work(nbytes: int, device):
+    import torch
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes > 0 else None
+
+
+def _ptr(t):
+    return _null() if t is None else ctypes.c_void_p(t.data_ptr())
+
+
+def gtp_layer_norm(x, L: int, w=None, b=None, eps: float = 1e-5, y=None, mean=None, rstd=None, stream=None):
+    """(y, mean, rstd): SH features x[N, C, (L+1)^2] normalised by degree (L = 0: the ordinary layer norm over C),
+    scaled by w[L+1, C] and, at degree 0, shifted by b[C] (fp32 or None); y has x's type, mean[N] and rstd[N, L+1]
+    fp32 are what the backward reads.  y may be x."""
+    import torch
+    if x.dim() != 3 or x.shape[2] != nsh(L):
+        raise ValueError("x must be [N, C, (L+1)^2]")
+    N, C = int(x.shape[0]), int(x.shape[1])
+    code = _dtype_code(x)
+    px = _want(x, "x", x.shape, _inputs())
+    pw = _opt(w, "w", (L + 1, C), _f32(), x.device)
+    pb = _opt(b, "b", (C,), _f32(), x.device)
+    with _on_stream(stream):
+        y = torch.empty_like(x) if y is None else y
+        mean = torch.empty(N, dtype=torch.float32, device=x.device) if mean is None else mean
+        rstd = torch.empty((N, L + 1), dtype=torch.float32, device=x.device) if rstd is None else rstd
+    py = _want(y, "y", x.shape, (x.dtype,), x.device)
+    pm = _want(mean, "mean", (N,), _f32(), x.device)
+    pr = _want(rstd, "rstd", (N, L + 1), _f32(), x.device)
+    _on_gpu(x, "x")
+    _check(lib().gtp_layer_norm(L, px, code, pw, pb, eps, N, C, py, pm, pr, _stream(stream)))
+    return y, mean, rstd
+
+
+def gtp_layer_norm_backward(x, dy, L: int, mean, rstd, w=None, need=("dx", "dw", "db"), stream=None):
+    """Gradients of <dy, gtp_layer_norm(x, L, w, b)>: a dict with the requested keys among dx (like x), dw[L+1, C] and
+    db[C] (fp32); mean, rstd as gtp_layer_norm returned them."""
+    import torch
+    if x.dim() != 3 or x.shape[2] != nsh(L):
+        raise ValueError("x must be [N, C, (L+1)^2]")
+    unknown = set(need) - {"dx", "dw", "db"}
+    if unknown:
+        raise ValueError(f"unknown gradients {sorted(unknown)}")
+    N, C = int(x.shape[0]), int(x.shape[1])
+    code = _dtype_code(x)
+    px = _want(x, "x", x.shape, _inputs())
+    pdy = _want(dy, "dy", x.shape, (x.dtype,), x.device)
+    pw = _opt(w, "w", (L + 1, C), _f32(), x.device)
+    pm = _want(mean, "mean", (N,), _f32(), x.device)
+    pr = _want(rstd, "rstd", (N, L + 1), _f32(), x.device)
+    _on_gpu(x, "x")
+    out = {}
+    with _on_stream(stream):
+        if "dx" in need:
+            out["dx"] = torch.empty_like(x)
+        if "dw" in need:
+            out["dw"] = torch.empty((L + 1, C), dtype=torch.float32, device=x.device)
+        if "db" in need:
+            out["db"] = torch.empty(C, dtype=torch.float32, device=x.device)
+        nbytes = lib().gtp_layer_norm_backward_work(L, code, N, C) if "dw" in need or "db" in need else 0
+        work = _work(nbytes, x.device)
+    _check(lib().gtp_layer_norm_backward(L, px, code, pw, pm, pr, pdy, N, C, _ptr(out.get("dx")), _ptr(out.get("dw")),
+                                         _ptr(out.get("db")), _ptr(work), nbytes, _stream(stream)))
+    return out
+
+
+def gtp_dropout(x, p: float, rng, res=None, y=None, stream=None):
+    """y = res + keep x / (1 - p), one draw for each row of x's last dimension (x[..., K]: the K coefficients of a
+    channel together; K = 1 drops single values).  rng: int64[2] on the device, (seed, offset), read when the call
+    runs; another offset gives other draws.  The gradient is the same call on dy, without res.  y may be x or res."""
+    import torch
+    if x.dim() < 1:
+        raise ValueError("x must have a last dimension")
+    code = _dtype_code(x)
+    K = int(x.shape[-1])
+    groups = x.numel() // K if K else 0
+    px = _want(x, "x", x.shape, _inputs())
+    pres = _opt(res, "res", x.shape, (x.dtype,), x.device)
+    prng = _rng_state(rng, x.device)
+    with _on_stream(stream):
+        y = torch.empty_like(x) if y is None else y
+    py = _want(y, "y", x.shape, (x.dtype,), x.device)
+    _on_gpu(x, "x")
+    _check(lib().gtp_dropout(px, pres, code, p, prng, groups, K, py, _stream(stream)))
+    return y
+
+
+def _attn_rows(t, name, shape, dtype, device):
+    """gtp_rows of a [rows, heads, d] tensor whose last dimension is contiguous (a slice of a packed tensor, or an
+    expanded input, will do)."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}; expected {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}; expected {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}; the other operands are on {device}")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _attn(q, k, v, scale, q_off, k_off, max_q, max_k, key_mask, p, rng):
+    """Validated gtp_attn and the rows of q, k, v."""
+    import torch
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q must be [Tq, H, d], k and v [Tk, Hk, d]")
+    code = _dtype_code(q)
+    Tq, H, d = (int(i) for i in q.shape)
+    Tk, Hk = int(k.shape[0]), int(k.shape[1])
+    i64 = (torch.int64,)
+    if H < 1 or Hk < 1 or d < 1 or H % Hk:
+        raise ValueError("the number of query heads must be a positive multiple of the number of key heads")
+    rows = [_attn_rows(q, "q", (Tq, H, d), q.dtype, q.device), _attn_rows(k, "k", (Tk, Hk, d), q.dtype, q.device),
+            _attn_rows(v, "v", (Tk, Hk, d), q.dtype, q.device)]
+    B = None
+    for off, name in ((q_off, "q_off"), (k_off, "k_off")):
+        if off is None:
+            continue
+        if off.dim() != 1 or off.shape[0] < 1:
+            raise ValueError(f"{name} must be [B + 1]")
+        if B is not None and off.shape[0] != B + 1:
+            raise ValueError("q_off and k_off must have one length")
+        B = int(off.shape[0]) - 1
+    if B is None:
+        # equal segments: of max_q and max_k rows, or one of all rows
+        n, most = (Tq, max_q) if max_q is not None else (Tk, max_k)
+        B = 1 if most is None else (n // most if most else 1)
+    max_q = (Tq if q_off is not None else Tq // max(B, 1)) if max_q is None else int(max_q)
+    max_k = (Tk if k_off is not None else Tk // max(B, 1)) if max_k is None else int(max_k)
+    desc = _Attn(code, H, Hk, d, B, Tq, Tk, min(max_q, Tq), min(max_k, Tk), _opt(q_off, "q_off", (B + 1,), i64, q.device),
+                 _opt(k_off, "k_off", (B + 1,), i64, q.device),
+                 _opt(key_mask, "key_mask", (Tk,), (torch.uint8, torch.bool), q.device),
+                 1.0 / d ** 0.5 if scale is None else scale, p, _null() if rng is None else _rng_state(rng, q.device))
+    return desc, rows
+
+
+def gtp_attention(q, k, v, scale=None, q_off=None, k_off=None, max_q=None, max_k=None, key_mask=None, p: float = 0.0,
+                  rng=None, o=None, lse=None, stream=None):
+    """(o, lse): softmax attention of q[Tq, H, d] over k, v[Tk, Hk, d] (H a multiple of Hk, d <= 256) within each
+    segment (molecule).  q_off, k_off: int64[B+1] device offsets of the segments' rows, max_q and max_k their longest
+    (host integers; left out, the whole tensor's length is taken, which costs idle workgroups); without offsets:
+    equal segments of max_q and max_k rows, or one.  key_mask[Tk]: 0 = absent key.  scale: 1 / sqrt(d) by default.
+    Probabilities are dropped with probability p by the generator state rng (see gtp_dropout).  lse[Tq, H] fp32 is
+    what the backward reads.  Tensors may be slices of a packed one (contiguous last dimension)."""
+    import torch
+    desc, rows = _attn(q, k, v, scale, q_off, k_off, max_q, max_k, key_mask, p, rng)
+    with _on_stream(stream):
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if o is None else o
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
+        ro = _attn_rows(o, "o", q.shape, q.dtype, q.device)
+        pl = _want(lse, "lse", q.shape[:2], _f32(), q.device)
+        _on_gpu(q, "q")
+        nbytes = lib().gtp_attention_work(ctypes.byref(desc), 0)
+        work = _work(nbytes, q.device)
+    _check(lib().gtp_attention(ctypes.byref(desc), *map(ctypes.byref, rows), ctypes.byref(ro), pl, _ptr(work), nbytes,
+                               _stream(stream)))
+    return o, lse
+
+
+def gtp_attention_backward(q, k, v, o, do, lse, scale=None, q_off=None, k_off=None, max_q=None, max_k=None,
+                           key_mask=None, p: float = 0.0, rng=None, need=("dq", "dk", "dv"), dq=None, dk=None, dv=None,
+                           stream=None):
+    """Gradients of <do, gtp_attention(q, k, v, ...)[0]>: a dict with the requested keys among dq, dk, dv (dk and dv
+    go together).  o, lse as the forward returned them, the other arguments as it had them.  dq, dk, dv: tensors to
+    write to (slices of a packed one will do)."""
+    import torch
+    desc, rows = _attn(q, k, v, scale, q_off, k_off, max_q, max_k, key_mask, p, rng)
+    need = set(need)
+    if need - {"dq", "dk", "dv"}:
+        raise ValueError(f"unknown gradients {sorted(need - {'dq', 'dk', 'dv'})}")
+    ro = _attn_rows(o, "o", q.shape, q.dtype, q.device)
+    rdo = _attn_rows(do, "do", q.shape, q.dtype, q.device)
+    pl = _want(lse, "lse", q.shape[:2], _f32(), q.device)
+    with _on_stream(stream):
+        out = {}
+        for name, like, given in (("dq", q, dq), ("dk", k, dk), ("dv", v, dv)):
+            if name in need or (name != "dq" and need & {"dk", "dv"}):
+                out[name] = torch.empty(like.shape, dtype=q.dtype, device=q.device) if given is None else given
+        ptr = {n: _attn_rows(out[n], n, t.shape, q.dtype, q.device) if n in out else None
+               for n, t in (("dq", q), ("dk", k), ("dv", v))}
+        _on_gpu(q, "q")
+        nbytes = lib().gtp_attention_work(ctypes.byref(desc), 1)
+        work = _work(nbytes, q.device)
+    _check(lib().gtp_attention_backward(ctypes.byref(desc), *map(ctypes.byref, rows), ctypes.byref(ro),
+                                        ctypes.byref(rdo), pl,
+                                        *(_null() if ptr[n] is None else ctypes.byref(ptr[n]) for n in ("dq", "dk", "dv")),
+                                        _ptr(work), nbytes, _stream(stream)))
+    return {n: out[n] for n in out if n in need}
 
 
 def gtp_stream_probe(mode: int, src, dst, stream=None):
