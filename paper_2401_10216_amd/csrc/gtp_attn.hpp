@@ -23,7 +23,8 @@ struct AttnArgs {
   const uint8_t* mask;           // [Tk] or null
   float* lse;                    // [Tq, H]: written by the forward, read by the backward
   float* delta;                  // [Tq, H]: rows' sums of dout o
-  float* part;                   // partial results of split calls
+  float* part;                   // results of the parts of a split call, [splits, rows, d] (forward: then [splits, rows]
+                                 // of lse; dk, dv: one behind the other)
   const uint64_t* rng;           // {seed, offset}, with threshold > 0
   int64_t B, Tq, Tk, max_q, max_k;
   int H, Hk, G, d;               // query heads, key heads, H / Hk, head length
@@ -35,9 +36,16 @@ struct AttnArgs {
 };
 
 int attn_padded(int d);  // the head length that the kernels are instantiated at, >= d
+// Parts that the keys of each row (the rows of each key) are dealt to: 1 where the
+// workgroups fill the chip without.
+int attn_row_splits(const AttnArgs& a);
+int attn_key_splits(const AttnArgs& a);
 hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_delta(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_dq(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_dkv(const AttnArgs& a, hipStream_t s);
+// Sums the parts of dq (keys = false), dk or dv (keys = true) into out.
+hipError_t launch_attn_sum(const AttnArgs& a, const float* part, int splits, bool keys, const AttnRows& out,
+                           hipStream_t s);
 
 }  // namespace gtp

@@ -34,6 +34,9 @@ constexpr float kLn2 = 0.6931471805599453f;
 // Row r of a wave's 32 x 32 result in register r (0..15) of lane half hi.
 __device__ __forceinline__ constexpr int tile_row(int r, int hi) { return 8 * (r >> 2) + 4 * hi + (r & 3); }
 
+// 2^x by the hardware's exponential (1 unit in the last place; results below 2^-126 are zero).
+__device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
+
 __device__ __forceinline__ f32x16 zero16() {
   f32x16 z;
 #pragma unroll
@@ -256,6 +259,11 @@ struct Drop {
     return keep;
   }
 };
+
+// Parts of a split call: part s of element (row, i), rows counted over all heads.
+__device__ __forceinline__ float* part_row(float* part, int split, int64_t rows, int64_t row, int d) {
+  return part + (int64_t(split) * rows + row) * d;
+}
 
 // Work of a workgroup: tiles fastest, then splits, key heads, segments; XCD-aware,
 // so that the workgroups that read one segment's rows share an L2.

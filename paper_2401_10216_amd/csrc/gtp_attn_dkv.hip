@@ -89,7 +89,7 @@ __global__ __launch_bounds__(NT) void k_attn_dkv(const AttnArgs a, int64_t n_wg,
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = 4 * g + i;
-        const float e = exp2f(fmaf(s[r], a.scale2, -rf[i]));
+        const float e = pow2(fmaf(s[r], a.scale2, -rf[i]));
         if constexpr (DROP) {
           const bool kept = (keep >> r) & 1u;
           p[r] = kept ? e : 0.0f;
@@ -117,6 +117,13 @@ __global__ __launch_bounds__(NT) void k_attn_dkv(const AttnArgs a, int64_t n_wg,
   if (!present)
 #pragma unroll
     for (int i = 0; i < NDT; ++i) ak[i] = zero16(), av[i] = zero16();
+  if (a.splits > 1) {
+    const int64_t all = a.Tk * a.Hk, row = (ks + j) * a.Hk + w.hk;
+    store_columns<float>(part_row(a.part, w.split, all, row, a.d), ak, a.scale, part * DO, a.d, hi, a.d % 4 == 0);
+    store_columns<float>(part_row(a.part + a.splits * all * a.d, w.split, all, row, a.d), av, DROP ? a.keep : 1.0f,
+                         part * DO, a.d, hi, a.d % 4 == 0);
+    return;
+  }
   if (a.dk.p)
     store_columns<T>(static_cast<T*>(const_cast<void*>(a.dk.p)) + (ks + j) * a.dk.row + w.hk * a.dk.head, ak, a.scale,
                      part * DO, a.d, hi, a.vec);

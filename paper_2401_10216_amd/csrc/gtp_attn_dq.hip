@@ -90,7 +90,7 @@ __global__ __launch_bounds__(NT) void k_attn_dq(const AttnArgs a, int64_t n_wg, 
     if constexpr (DROP) keep = drop.keys_of_row(R, j0, hi);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const float p = exp2f(fmaf(s[r], a.scale2, -ref));
+      const float p = pow2(fmaf(s[r], a.scale2, -ref));
       const float g = DROP ? ((keep >> r) & 1u ? dp[r] * a.keep : 0.0f) : dp[r];
       s[r] = (ok >> tile_row(r, 0)) & 1u ? p * (g - delta) : 0.0f;
     }
@@ -98,6 +98,11 @@ __global__ __launch_bounds__(NT) void k_attn_dq(const AttnArgs a, int64_t n_wg, 
     for (int i = 0; i < NDT; ++i) mma_transposed<T, DP>(tk, i, s, lane, acc[i]);
   }
   if (!there) return;
+  if (a.splits > 1) {
+    store_columns<float>(part_row(a.part, w.split, a.Tq * a.H, qi * a.H + h, a.d), acc, a.scale, 0, a.d, hi,
+                         a.d % 4 == 0);
+    return;
+  }
   store_columns<T>(static_cast<T*>(const_cast<void*>(a.out.p)) + qi * a.out.row + h * a.out.head, acc, a.scale, 0, a.d,
                    hi, a.vec);
 }

@@ -73,7 +73,7 @@ __global__ __launch_bounds__(NT) void k_attn_fwd(const AttnArgs a, int64_t n_wg,
     top = fmaxf(top, __shfl_xor(top, 32));
     const float m_new = fmaxf(m, top);
     const float ref = m_new == -INFINITY ? 0.0f : m_new;  // no score yet: every exponential below is zero
-    const float f = exp2f(m - ref);
+    const float f = pow2(m - ref);
     m = m_new;
     l *= f;
 #pragma unroll
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(NT) void k_attn_fwd(const AttnArgs a, int64_t n_wg,
       if constexpr (DROP) keep = drop.keys_of_row(R, j0 + 32 * t, hi);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float p = exp2f(s[t][r] - ref);
+        const float p = pow2(s[t][r] - ref);
         l += p;
         s[t][r] = DROP && !((keep >> r) & 1u) ? 0.0f : p;
       }
@@ -96,9 +96,94 @@ __global__ __launch_bounds__(NT) void k_attn_fwd(const AttnArgs a, int64_t n_wg,
   l += __shfl_xor(l, 32);
   if (!there) return;
   const float inv = l == 0.0f ? 0.0f : (DROP ? a.keep / l : 1.0f / l);
+  const float lse = l == 0.0f ? -INFINITY : m * kLn2 + logf(l);
+  if (a.splits > 1) {
+    const int64_t all = a.Tq * a.H, row = qi * a.H + h;
+    store_columns<float>(part_row(a.part, w.split, all, row, a.d), acc, inv, 0, a.d, hi, a.d % 4 == 0);
+    if (hi == 0) a.part[a.splits * all * a.d + w.split * all + row] = lse;
+    return;
+  }
   store_columns<T>(static_cast<T*>(const_cast<void*>(a.out.p)) + qi * a.out.row + h * a.out.head, acc, inv, 0, a.d, hi,
                    a.vec);
-  if (hi == 0) a.lse[qi * a.H + h] = l == 0.0f ? -INFINITY : m * kLn2 + logf(l);
+  if (hi == 0) a.lse[qi * a.H + h] = lse;
+}
+
+// Joins the parts of a split forward: o = sum_s e^(lse_s - lse) o_s.  A wave takes a
+// row, its lanes first the parts, then the elements.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a) {
+  const int64_t per = (a.max_q * a.H + 3) / 4, b = blockIdx.x / per;
+  const int64_t i = (blockIdx.x % per) * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  int64_t qs, nq;
+  segment(a.q_off, b, a.max_q, a.Tq, qs, nq);
+  if (i >= nq * a.H) return;
+  const int64_t t = qs + i / a.H, h = i % a.H, all = a.Tq * a.H, row = t * a.H + h;
+  const float* const lses = a.part + a.splits * all * a.d;
+  const float own = lane < a.splits ? lses[lane * all + row] : -INFINITY;
+  float top = own;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  const float e = own == -INFINITY ? 0.0f : expf(own - top);  // NaN where a part's row is
+  float sum = e;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  const float weight = sum == 0.0f ? 0.0f : e / sum;
+  if (lane == 0) a.lse[row] = sum == 0.0f ? -INFINITY : top + logf(sum);
+  T* const out = static_cast<T*>(const_cast<void*>(a.out.p)) + t * a.out.row + h * a.out.head;
+  for (int c0 = 0; c0 < a.d; c0 += 64) {
+    const int c = c0 + lane;
+    float v = 0.0f;
+#pragma unroll 8
+    for (int s = 0; s < a.splits; ++s) {
+      const float ws = __shfl(weight, s);
+      const float p = c < a.d ? a.part[(int64_t(s) * all + row) * a.d + c] : 0.0f;
+      v = ws == 0.0f ? v : fmaf(ws, p, v);
+    }
+    if (c < a.d) {
+      if constexpr (sizeof(T) == 4) {
+        out[c] = v;
+      } else {
+        const __bf16 one = static_cast<__bf16>(v);
+        out[c] = __builtin_bit_cast(uint16_t, one);
+      }
+    }
+  }
+}
+
+// Sums the parts of a split gradient, in order, a wave a row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_sum(const float* __restrict__ part, int splits, const int64_t* off,
+                                                  int64_t most, int64_t total, int heads, int d, AttnRows out) {
+  const int64_t per = (most * heads + 3) / 4, b = blockIdx.x / per;
+  const int64_t i = (blockIdx.x % per) * 4 + (threadIdx.x >> 6);
+  int64_t start, n;
+  segment(off, b, most, total, start, n);
+  if (i >= n * heads) return;
+  const int64_t t = start + i / heads, h = i % heads, all = total * heads, row = t * heads + h;
+  T* const o = static_cast<T*>(const_cast<void*>(out.p)) + t * out.row + h * out.head;
+  for (int c = threadIdx.x & 63; c < d; c += 64) {
+    float v = 0.0f;
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) v += part[(int64_t(s) * all + row) * d + c];
+    if constexpr (sizeof(T) == 4) {
+      o[c] = v;
+    } else {
+      const __bf16 one = static_cast<__bf16>(v);
+      o[c] = __builtin_bit_cast(uint16_t, one);
+    }
+  }
+}
+
+constexpr int64_t kFill = 768;  // workgroups, three a CU
+
+// Parts for n workgroups whose loops take `tiles` tiles: enough for kFill
+// workgroups, two tiles each at least.
+int parts_for(int64_t n, int64_t tiles) {
+  if (n <= 0 || n >= kFill / 2) return 1;
+  int64_t s = (kFill + n - 1) / n;
+  if (s > tiles / 2) s = tiles / 2;
+  return s < 1 ? 1 : s > 64 ? 64 : int(s);
 }
 
 template <typename T, int DP>
@@ -109,12 +194,37 @@ hipError_t launch(const AttnArgs& a, hipStream_t s) {
     k_attn_fwd<T, DP, KT, true><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
   else
     k_attn_fwd<T, DP, KT, false><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
+  if (a.splits > 1) {
+    const int64_t rows = (a.max_q * a.H + 3) / 4 * a.B;
+    k_attn_join<T><<<uint32_t(rows), 256, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
 int attn_padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256; }
+
+int attn_row_splits(const AttnArgs& a) {
+  return parts_for((a.max_q * a.G + BM - 1) / BM * a.Hk * a.B, (a.max_k + 63) / 64);
+}
+int attn_key_splits(const AttnArgs& a) {
+  return parts_for((a.max_k + 127) / 128 * a.Hk * a.B, (a.max_q * a.G + 63) / 64);
+}
+
+hipError_t launch_attn_sum(const AttnArgs& a, const float* part, int splits, bool keys, const AttnRows& out,
+                           hipStream_t s) {
+  const int64_t* off = keys ? a.k_off : a.q_off;
+  const int64_t most = keys ? a.max_k : a.max_q, total = keys ? a.Tk : a.Tq;
+  const int heads = keys ? a.Hk : a.H;
+  const uint32_t n = uint32_t((most * heads + 3) / 4 * a.B);
+  if (n == 0) return hipSuccess;
+  if (a.bf16)
+    k_attn_sum<uint16_t><<<n, 256, 0, s>>>(part, splits, off, most, total, heads, a.d, out);
+  else
+    k_attn_sum<float><<<n, 256, 0, s>>>(part, splits, off, most, total, heads, a.d, out);
+  return hipGetLastError();
+}
 
 hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t s) {
   switch (attn_padded(a.d)) {

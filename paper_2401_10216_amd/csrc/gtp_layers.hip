@@ -260,7 +260,15 @@ gtp_status attn_sizes(const gtp_attn* a, gtp::AttnArgs* g) {
 
 gtp::AttnRows rows_of(const gtp_rows* r) { return r ? gtp::AttnRows{r->data, r->row, r->head} : gtp::AttnRows{}; }
 
-int64_t attn_work(const gtp::AttnArgs& g, int backward) { return backward ? (g.Tq * g.H * 4 + 15) / 16 * 16 : 0; }
+// The forward: the parts of a split call and their lse.  The backward: the rows'
+// deltas, then the parts of dq or of dk and dv, one after the other in the same place.
+int64_t delta_bytes(const gtp::AttnArgs& g) { return (g.Tq * g.H * 4 + 15) / 16 * 16; }
+int64_t attn_work(const gtp::AttnArgs& g, int backward) {
+  const int64_t s = gtp::attn_row_splits(g), rows = s > 1 ? s * g.Tq * g.H * (g.d + (backward ? 0 : 1)) * 4 : 0;
+  if (!backward) return rows;
+  const int64_t t = gtp::attn_key_splits(g), keys = t > 1 ? 2 * t * g.Tk * g.Hk * g.d * 4 : 0;
+  return delta_bytes(g) + (rows > keys ? rows : keys);
+}
 
 // Checks of `n` inputs and outputs against each other, the row statistics, the
 // work and the index arrays.
@@ -332,6 +340,7 @@ gtp_status gtp_attention(const gtp_attn* a, const gtp_rows* q, const gtp_rows* k
   g.out = rows_of(o);
   g.lse = lse;
   g.part = static_cast<float*>(work);
+  g.splits = gtp::attn_row_splits(g);
   return launched(gtp::launch_attn_fwd(g, static_cast<hipStream_t>(stream)), "gtp_attention");
 }
 
@@ -363,8 +372,19 @@ gtp_status gtp_attention_backward(const gtp_attn* a, const gtp_rows* q, const gt
   g.delta = static_cast<float*>(work);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = a->Tq > 0 ? gtp::launch_attn_delta(g, st) : hipSuccess;
-  if (e == hipSuccess && dq && a->max_q > 0) e = gtp::launch_attn_dq(g, st);
-  if (e == hipSuccess && dk && a->max_k > 0) e = gtp::launch_attn_dkv(g, st);
+  g.part = reinterpret_cast<float*>(static_cast<char*>(work) + delta_bytes(g));
+  if (e == hipSuccess && dq && a->max_q > 0) {
+    g.splits = gtp::attn_row_splits(g);
+    e = gtp::launch_attn_dq(g, st);
+    if (e == hipSuccess && g.splits > 1) e = gtp::launch_attn_sum(g, g.part, g.splits, false, g.out, st);
+  }
+  if (e == hipSuccess && dk && a->max_k > 0) {
+    g.splits = gtp::attn_key_splits(g);
+    e = gtp::launch_attn_dkv(g, st);
+    const int64_t one = g.splits * g.Tk * g.Hk * g.d;
+    if (e == hipSuccess && g.splits > 1) e = gtp::launch_attn_sum(g, g.part, g.splits, true, g.dk, st);
+    if (e == hipSuccess && g.splits > 1) e = gtp::launch_attn_sum(g, g.part + one, g.splits, true, g.dv, st);
+  }
   return launched(e, "gtp_attention_backward");
 }
 
