@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "gtp_attn.hpp"
 #include "gtp_device.hpp"
@@ -42,6 +43,18 @@ __device__ __forceinline__ f32x16 zero16() {
 #pragma unroll
   for (int i = 0; i < 16; ++i) z[i] = 0.0f;
   return z;
+}
+
+// max(v, v of lane ^ 32) and their sum.
+__device__ __forceinline__ float half_max(float v) {
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
 // acc += A B over the 32 bytes of the summed axis (8 fp32 or 16 bf16 values)
@@ -224,41 +237,78 @@ struct Drop {
     const uint64_t nr = uint64_t(a.max_q * a.G + 3) >> 2;
     base = (uint64_t(b) * a.Hk + hk) * nr * nc;
   }
-  // Bit r of the result: whether element (row R, key j0 + tile_row(r, hi)) is kept.
-  __device__ __forceinline__ uint32_t keys_of_row(int64_t R, int64_t j0, int hi) const {
-    uint32_t keep = 0;
+  // The draws of a 32 x 32 tile whose first row is R0 and first key j0, in the two
+  // layouts of a result.  A lane's run of four elements (register group g) is one row
+  // or column of a block; the four lanes of a quad need the same four blocks, so lane
+  // q makes the two calls of block g = q alone and they trade: 16 draws a lane cost two
+  // calls, not eight.
+  //
+  // Bit r: whether element (row R0 + lane & 31, key j0 + tile_row(r, hi)) is kept.
+  __device__ __forceinline__ uint32_t keys_of_row(int64_t R0, int64_t j0, int lane) const {
+    const int q = lane & 3;
+    const uint64_t block =
+        base + uint64_t((R0 + (lane & 28)) >> 2) * nc + uint64_t((j0 + 8 * q + 4 * (lane >> 5)) >> 2);
+    uint32_t bits = 0;  // of block q: nibble r = row r's four keys
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const uint64_t block = base + uint64_t(R >> 2) * nc + uint64_t((j0 + 8 * g + 4 * hi) >> 2);
+    for (int h = 0; h < 2; ++h) {
       uint32_t w[4];
-      philox(2 * block + ((R >> 1) & 1), seed, offset, w);
-      const uint32_t a = (R & 1) ? w[2] : w[0], b = (R & 1) ? w[3] : w[1];
-      keep |= ((a & 0xffffu) >= threshold ? 1u : 0u) << (4 * g);
-      keep |= ((a >> 16) >= threshold ? 1u : 0u) << (4 * g + 1);
-      keep |= ((b & 0xffffu) >= threshold ? 1u : 0u) << (4 * g + 2);
-      keep |= ((b >> 16) >= threshold ? 1u : 0u) << (4 * g + 3);
+      philox(2 * block + h, seed, offset, w);
+      bits |= kept8(w) << (8 * h);
     }
-    return keep;
+    return trade(bits, q);
   }
-  // Bit r: whether element (row R0 + tile_row(r, hi), key j) is kept.
-  __device__ __forceinline__ uint32_t rows_of_key(int64_t j, int64_t R0, int hi) const {
-    uint32_t keep = 0;
+  // Bit r: whether element (row R0 + tile_row(r, hi), key j0 + lane & 31) is kept.
+  __device__ __forceinline__ uint32_t rows_of_key(int64_t R0, int64_t j0, int lane) const {
+    const int q = lane & 3;
+    const uint64_t block =
+        base + uint64_t((R0 + 8 * q + 4 * (lane >> 5)) >> 2) * nc + uint64_t((j0 + (lane & 28)) >> 2);
+    uint32_t bits = 0;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const uint64_t block = base + uint64_t((R0 + 8 * g + 4 * hi) >> 2) * nc + uint64_t(j >> 2);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t w[4];
-        philox(2 * block + h, seed, offset, w);
-        const uint32_t a = (j & 2) ? w[1] : w[0], b = (j & 2) ? w[3] : w[2];
-        const int sh = 16 * int(j & 1);
-        keep |= (((a >> sh) & 0xffffu) >= threshold ? 1u : 0u) << (4 * g + 2 * h);
-        keep |= (((b >> sh) & 0xffffu) >= threshold ? 1u : 0u) << (4 * g + 2 * h + 1);
-      }
+    for (int h = 0; h < 2; ++h) {
+      uint32_t w[4];
+      philox(2 * block + h, seed, offset, w);
+      bits |= kept8(w) << (8 * h);
     }
-    return keep;
+    // the 4 x 4 bits turned over: nibble j = key j's four rows
+    uint32_t t = (bits ^ (bits >> 3)) & 0x0a0au;
+    bits ^= t ^ (t << 3);
+    t = (bits ^ (bits >> 6)) & 0x00ccu;
+    bits ^= t ^ (t << 6);
+    return trade(bits, q);
+  }
+  // Bit h: whether draw h of a call keeps.
+  __device__ __forceinline__ uint32_t kept8(const uint32_t (&w)[4]) const {
+    uint32_t b = 0;
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      b |= ((w[h] & 0xffffu) >= threshold ? 1u : 0u) << (2 * h);
+      b |= ((w[h] >> 16) >= threshold ? 1u : 0u) << (2 * h + 1);
+    }
+    return b;
+  }
+  // Lane q of a quad holds block q's nibbles; it gets nibble q of each block g, at bits 4 g.
+  __device__ __forceinline__ static uint32_t trade(uint32_t bits, int q) {
+    uint32_t out = 0;
+    auto take = [&](auto ctrl, int g) {
+      const uint32_t b = uint32_t(
+          __builtin_amdgcn_update_dpp(0, int(bits), decltype(ctrl)::value, 0xf, 0xf, true));
+      out |= ((b >> (4 * q)) & 0xfu) << (4 * g);
+    };
+    take(std::integral_constant<int, 0x00>{}, 0);  // quad_perm 0 0 0 0
+    take(std::integral_constant<int, 0x55>{}, 1);  // 1 1 1 1
+    take(std::integral_constant<int, 0xaa>{}, 2);
+    take(std::integral_constant<int, 0xff>{}, 3);
+    return out;
   }
 };
+
+// Waves a SIMD that a kernel's registers are cut for: two hide each other's
+// waits (one issues vector instructions while the matrix unit works for the
+// other), where rows, accumulators and a prefetched tile fit 256 registers.
+template <typename T, int DP>
+constexpr int waves_per_simd() {
+  return DP * int(sizeof(T)) <= 256 ? 2 : 1;
+}
 
 // Parts of a split call: part s of element (row, i), rows counted over all heads.
 __device__ __forceinline__ float* part_row(float* part, int split, int64_t rows, int64_t row, int d) {

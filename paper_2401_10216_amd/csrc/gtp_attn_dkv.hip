@@ -7,13 +7,19 @@
 namespace gtp {
 namespace {
 
+// Keys, values and both accumulators take twice what dq's rows do.
+template <typename T, int DP>
+constexpr int dkv_waves() {
+  return DP * int(sizeof(T)) <= 128 ? 2 : 1;
+}
+
 constexpr int NW = 4, NT = 64 * NW, BK = 32 * NW;
 
 // Workgroup: 128 keys of one key head (4 waves x 32), rows in tiles of 32.  Heads
 // longer than 128 are dealt to `parts` workgroups by output elements (DO each):
 // the accumulators of all of them would not fit the registers.
 template <typename T, int DP, int DO, bool DROP>
-__global__ __launch_bounds__(NT) void k_attn_dkv(const AttnArgs a, int64_t n_wg, int tiles) {
+__global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void k_attn_dkv(const AttnArgs a, int64_t n_wg, int tiles) {
   constexpr int BR = 32, NC = DP * int(sizeof(T)) / 32, NDT = DO / 32, PARTS = DP / DO;
   __shared__ __align__(16) char tq[BR * tile_stride<T, DP>()];
   __shared__ __align__(16) char tg[BR * tile_stride<T, DP>()];
@@ -52,20 +58,28 @@ __global__ __launch_bounds__(NT) void k_attn_dkv(const AttnArgs a, int64_t n_wg,
   const int64_t ntile = (rows + BR - 1) / BR, per = (ntile + a.splits - 1) / a.splits;
   const int64_t r_end = (w.split + 1) * per * BR < rows ? (w.split + 1) * per * BR : rows;
   Stage<T, DP, BR, NT> sq, sg;
-  for (int64_t r0 = w.split * per * BR; r0 < r_end; r0 += BR) {
+  float ref = INFINITY, delta = 0.0f;
+  auto fetch = [&](int64_t r0) {
     auto row = [&](const AttnRows& t, int r) -> const T* {
       const int64_t R = r0 + r;
-      return R < rows ? static_cast<const T*>(t.p) + (qs + R / a.G) * t.row + (w.hk * a.G + R % a.G) * t.head : nullptr;
+      if (R >= rows) return nullptr;
+      const int64_t i = a.G == 1 ? R : R / a.G, g = a.G == 1 ? 0 : R % a.G;
+      return static_cast<const T*>(t.p) + (qs + i) * t.row + (w.hk * a.G + g) * t.head;
     };
     sq.fetch([&](int r) { return row(a.q, r); }, a.d, a.vec);
     sg.fetch([&](int r) { return row(a.dout, r); }, a.d, a.vec);
-    float ref = INFINITY, delta = 0.0f;
+    ref = INFINITY;
+    delta = 0.0f;
     if (threadIdx.x < BR && r0 + threadIdx.x < rows) {
       const int64_t R = r0 + threadIdx.x, at = (qs + R / a.G) * a.H + w.hk * a.G + R % a.G;
       const float lse = a.lse[at];
       ref = lse == -INFINITY ? INFINITY : lse * kLog2e;
       delta = a.delta[at];
     }
+  };
+  int64_t r0 = w.split * per * BR;
+  if (r0 < r_end) fetch(r0);
+  for (; r0 < r_end; r0 += BR) {
     __syncthreads();
     sq.commit(tq);
     sg.commit(tg);
@@ -74,13 +88,14 @@ __global__ __launch_bounds__(NT) void k_attn_dkv(const AttnArgs a, int64_t n_wg,
       t_delta[threadIdx.x] = delta;
     }
     __syncthreads();
+    if (r0 + BR < r_end) fetch(r0 + BR);  // in flight while this tile is worked on
     f32x16 s = zero16(), dp = zero16();
 #pragma unroll
     for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tq, l31, c, hi), kf[c], s);
 #pragma unroll
     for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tg, l31, c, hi), vf[c], dp);
     uint32_t keep = 0xffffu;
-    if constexpr (DROP) keep = drop.rows_of_key(j, r0, hi);
+    if constexpr (DROP) keep = drop.rows_of_key(r0, int64_t(tile) * BK + wave * 32, lane);
     f32x16 p;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {

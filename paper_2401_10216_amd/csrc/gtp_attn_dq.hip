@@ -29,7 +29,7 @@ __global__ __launch_bounds__(256) void k_attn_delta(const AttnArgs a) {
 
 // Workgroup: 128 rows of one key head (4 waves x 32), keys in tiles of 32.
 template <typename T, int DP, bool DROP>
-__global__ __launch_bounds__(NT) void k_attn_dq(const AttnArgs a, int64_t n_wg, int tiles) {
+__global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_dq(const AttnArgs a, int64_t n_wg, int tiles) {
   constexpr int BN = 32, NC = DP * int(sizeof(T)) / 32, NDT = DP / 32;
   __shared__ __align__(16) char tk[BN * tile_stride<T, DP>()];
   __shared__ __align__(16) char tv[BN * tile_stride<T, DP>()];
@@ -42,7 +42,7 @@ __global__ __launch_bounds__(NT) void k_attn_dq(const AttnArgs a, int64_t n_wg, 
   const int64_t rows = nq * a.G;
   if (int64_t(w.tile) * BM >= rows) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l31 = lane & 31, hi = lane >> 5;
-  const int64_t R = int64_t(w.tile) * BM + wave * 32 + l31;
+  const int64_t R0 = int64_t(w.tile) * BM + wave * 32, R = R0 + l31;
   const bool there = R < rows;
   const int64_t qi = there ? qs + R / a.G : 0;
   const int h = w.hk * a.G + (there ? int(R % a.G) : 0);
@@ -72,27 +72,36 @@ __global__ __launch_bounds__(NT) void k_attn_dq(const AttnArgs a, int64_t n_wg, 
   const int64_t ntile = (nk + BN - 1) / BN, per = (ntile + a.splits - 1) / a.splits;
   const int64_t j_end = (w.split + 1) * per * BN < nk ? (w.split + 1) * per * BN : nk;
   Stage<T, DP, BN, NT> sk, sv;
-  for (int64_t j0 = w.split * per * BN; j0 < j_end; j0 += BN) {
-    auto present = [&](int r) { return j0 + r < nk && (!mask || mask[j0 + r]); };
-    sk.fetch([&](int r) { return present(r) ? kb + (j0 + r) * a.k.row : nullptr; }, a.d, a.vec);
-    sv.fetch([&](int r) { return present(r) ? vb + (j0 + r) * a.v.row : nullptr; }, a.d, a.vec);
+  auto present = [&](int64_t j) { return j < nk && (!mask || mask[j]); };
+  auto fetch = [&](int64_t j0) {
+    sk.fetch([&](int r) { return present(j0 + r) ? kb + (j0 + r) * a.k.row : nullptr; }, a.d, a.vec);
+    sv.fetch([&](int r) { return present(j0 + r) ? vb + (j0 + r) * a.v.row : nullptr; }, a.d, a.vec);
+  };
+  int64_t j0 = w.split * per * BN;
+  if (j0 < j_end) fetch(j0);
+  for (; j0 < j_end; j0 += BN) {
     __syncthreads();
     sk.commit(tk);
     sv.commit(tv);
     __syncthreads();
+    if (j0 + BN < j_end) fetch(j0 + BN);  // in flight while this tile is worked on
     f32x16 s = zero16(), dp = zero16();
 #pragma unroll
     for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tk, l31, c, hi), qf[c], s);
 #pragma unroll
     for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tv, l31, c, hi), gf[c], dp);
-    const uint32_t ok = uint32_t(__ballot(present(l31))) >> (4 * hi);
     uint32_t keep = 0xffffu;
-    if constexpr (DROP) keep = drop.keys_of_row(R, j0, hi);
+    if constexpr (DROP) keep = drop.keys_of_row(R0, j0, lane);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float p = pow2(fmaf(s[r], a.scale2, -ref));
       const float g = DROP ? ((keep >> r) & 1u ? dp[r] * a.keep : 0.0f) : dp[r];
-      s[r] = (ok >> tile_row(r, 0)) & 1u ? p * (g - delta) : 0.0f;
+      s[r] = p * (g - delta);
+    }
+    if (mask || j0 + BN > nk) {
+      const uint32_t ok = uint32_t(__ballot(present(j0 + l31))) >> (4 * hi);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = (ok >> tile_row(r, 0)) & 1u ? s[r] : 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < NDT; ++i) mma_transposed<T, DP>(tk, i, s, lane, acc[i]);

@@ -8,10 +8,11 @@ namespace gtp {
 namespace {
 
 constexpr int NW = 4, NT = 64 * NW, BM = 32 * NW;
+constexpr float kSlack = 8.0f;  // probabilities stay below 2^8: far from overflow in fp32 and bf16, and as exact
 
 // Workgroup: 128 rows of one key head (4 waves x 32), keys in tiles of 32 KT.
 template <typename T, int DP, int KT, bool DROP>
-__global__ __launch_bounds__(NT) void k_attn_fwd(const AttnArgs a, int64_t n_wg, int tiles) {
+__global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_fwd(const AttnArgs a, int64_t n_wg, int tiles) {
   constexpr int BN = 32 * KT, NC = DP * int(sizeof(T)) / 32, NDT = DP / 32;
   __shared__ __align__(16) char tk[BN * tile_stride<T, DP>()];
   __shared__ __align__(16) char tv[BN * tile_stride<T, DP>()];
@@ -24,20 +25,25 @@ __global__ __launch_bounds__(NT) void k_attn_fwd(const AttnArgs a, int64_t n_wg,
   const int64_t rows = nq * a.G;
   if (int64_t(w.tile) * BM >= rows) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l31 = lane & 31, hi = lane >> 5;
-  const int64_t R = int64_t(w.tile) * BM + wave * 32 + l31;
+  const int64_t R0 = int64_t(w.tile) * BM + wave * 32, R = R0 + l31;
   const bool there = R < rows;
   const int64_t qi = there ? qs + R / a.G : 0;
   const int h = w.hk * a.G + (there ? int(R % a.G) : 0);
+  // the scores' scale is taken positive, its sign into q: their maximum is then that of the products
+  const float scale2 = fabsf(a.scale2);
   u32x4 qf[NC];
   {
     const T* row = there ? static_cast<const T*>(a.q.p) + qi * a.q.row + h * a.q.head : nullptr;
+    const uint32_t flip = a.scale2 < 0.0f ? (sizeof(T) == 4 ? 0x80000000u : 0x80008000u) : 0u;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) qf[c] = load16<T>(row, 2 * c + hi, a.d, a.vec);
+    for (int c = 0; c < NC; ++c) qf[c] = load16<T>(row, 2 * c + hi, a.d, a.vec) ^ flip;
   }
   f32x16 acc[NDT];
 #pragma unroll
   for (int i = 0; i < NDT; ++i) acc[i] = zero16();
-  float m = -INFINITY, l = 0.0f;  // of the row's scores in units of log 2; this half's part of the sum
+  // m: the reference of the row's exponentials in units of log 2, at most kSlack below its largest score so far;
+  // l: this half's part of their sum
+  float m = -INFINITY, l = 0.0f;
   Drop drop;
   if constexpr (DROP) drop.init(a, w.b, w.hk);
 
@@ -47,53 +53,74 @@ __global__ __launch_bounds__(NT) void k_attn_fwd(const AttnArgs a, int64_t n_wg,
   const int64_t ntile = (nk + BN - 1) / BN, per = (ntile + a.splits - 1) / a.splits;
   const int64_t j_end = (w.split + 1) * per * BN < nk ? (w.split + 1) * per * BN : nk;
   Stage<T, DP, BN, NT> sk, sv;
-  for (int64_t j0 = w.split * per * BN; j0 < j_end; j0 += BN) {
-    // absent keys' rows are not read: zeros stand for them
-    auto present = [&](int r) { return j0 + r < nk && (!mask || mask[j0 + r]); };
-    sk.fetch([&](int r) { return present(r) ? kb + (j0 + r) * a.k.row : nullptr; }, a.d, a.vec);
-    sv.fetch([&](int r) { return present(r) ? vb + (j0 + r) * a.v.row : nullptr; }, a.d, a.vec);
+  // absent keys' rows are not read: zeros stand for them
+  auto present = [&](int64_t j) { return j < nk && (!mask || mask[j]); };
+  auto fetch = [&](int64_t j0) {
+    sk.fetch([&](int r) { return present(j0 + r) ? kb + (j0 + r) * a.k.row : nullptr; }, a.d, a.vec);
+    sv.fetch([&](int r) { return present(j0 + r) ? vb + (j0 + r) * a.v.row : nullptr; }, a.d, a.vec);
+  };
+  int64_t j0 = w.split * per * BN;
+  if (j0 < j_end) fetch(j0);
+  for (; j0 < j_end; j0 += BN) {
     __syncthreads();
     sk.commit(tk);
     sv.commit(tv);
     __syncthreads();
+    if (j0 + BN < j_end) fetch(j0 + BN);  // in flight while this tile is worked on
+    const bool whole = !mask && j0 + BN <= nk;
     f32x16 s[KT];
+    uint32_t ok[KT];
     float top = -INFINITY;
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
       s[t] = zero16();
 #pragma unroll
       for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tk, 32 * t + l31, c, hi), qf[c], s[t]);
-      const uint32_t ok = uint32_t(__ballot(present(32 * t + l31))) >> (4 * hi);
+    }
+    if (!whole) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[t][r] = (ok >> tile_row(r, 0)) & 1u ? s[t][r] * a.scale2 : -INFINITY;
-        top = fmaxf(top, s[t][r]);
+      for (int t = 0; t < KT; ++t) {
+        ok[t] = uint32_t(__ballot(present(j0 + 32 * t + l31))) >> (4 * hi);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = (ok[t] >> tile_row(r, 0)) & 1u ? s[t][r] : -INFINITY;
       }
     }
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float m_new = fmaxf(m, top);
-    const float ref = m_new == -INFINITY ? 0.0f : m_new;  // no score yet: every exponential below is zero
-    const float f = pow2(m - ref);
-    m = m_new;
-    l *= f;
 #pragma unroll
-    for (int i = 0; i < NDT; ++i) acc[i] *= f;
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
+    top = half_max(top) * scale2;
+    // the reference moves only where a score passes it by kSlack: the accumulators are seldom scaled
+    if (__any(top > m + kSlack)) {
+      const float m_new = fmaxf(m, top);
+      const float f = m_new == m ? 1.0f : pow2(m - m_new);
+      m = m_new;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < NDT; ++i) acc[i] *= f;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;  // no score yet: every exponential below is zero
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
       uint32_t keep = 0xffffu;
-      if constexpr (DROP) keep = drop.keys_of_row(R, j0 + 32 * t, hi);
+      if constexpr (DROP) keep = drop.keys_of_row(R0, j0 + 32 * t, lane);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[t][r] = pow2(fmaf(s[t][r], scale2, -ref));
+      if (!whole) {  // also where scale is 0
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = (ok[t] >> tile_row(r, 0)) & 1u ? s[t][r] : 0.0f;
+      }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float p = pow2(s[t][r] - ref);
-        l += p;
-        s[t][r] = DROP && !((keep >> r) & 1u) ? 0.0f : p;
+        l += s[t][r];
+        if constexpr (DROP) s[t][r] = (keep >> r) & 1u ? s[t][r] : 0.0f;
       }
 #pragma unroll
       for (int i = 0; i < NDT; ++i)
         mma_transposed<T, DP>(tv + 32 * t * tile_stride<T, DP>(), i, s[t], lane, acc[i]);
     }
   }
-  l += __shfl_xor(l, 32);
+  l = half_sum(l);
   if (!there) return;
   const float inv = l == 0.0f ? 0.0f : (DROP ? a.keep / l : 1.0f / l);
   const float lse = l == 0.0f ? -INFINITY : m * kLn2 + logf(l);
@@ -134,7 +161,6 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a) {
   for (int c0 = 0; c0 < a.d; c0 += 64) {
     const int c = c0 + lane;
     float v = 0.0f;
-#pragma unroll 8
     for (int s = 0; s < a.splits; ++s) {
       const float ws = __shfl(weight, s);
       const float p = c < a.d ? a.part[(int64_t(s) * all + row) * a.d + c] : 0.0f;
@@ -188,7 +214,7 @@ int parts_for(int64_t n, int64_t tiles) {
 
 template <typename T, int DP>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
-  constexpr int KT = DP * int(sizeof(T)) > 512 ? 1 : 2;
+  constexpr int KT = DP * int(sizeof(T)) > 256 ? 1 : 2;
   const int64_t tiles = (a.max_q * a.G + BM - 1) / BM, n = tiles * a.splits * a.Hk * a.B;
   if (a.threshold)
     k_attn_fwd<T, DP, KT, true><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
