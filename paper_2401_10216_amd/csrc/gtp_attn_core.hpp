@@ -57,68 +57,137 @@ __device__ __forceinline__ float half_sum(float v) {
   return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
-// acc += A B over the 32 bytes of the summed axis (8 fp32 or 16 bf16 values)
-// of which the lane holds its half's 16: A's of row lane & 31, B's of column
-// lane & 31.
+// fp32 operands go to the matrix unit in three bf16 parts, v = v1 + v2 + v3 (24
+// bits: exact down to 2^-110), a product as the six partial products of 2^-16 of it and
+// up: what is left out is below 2^-24 of a product, an fp32 rounding, and no value's
+// range matters, since bf16 has fp32's exponents.  Six 16-bit products of depth 16 take
+// 192 cycles, the fp32 instructions for that depth 512.  bf16 operands are one part.
 template <typename T>
-__device__ __forceinline__ void mma_chunk(const u32x4& a, const u32x4& b, f32x16& acc) {
-  if constexpr (sizeof(T) == 4) {
-    const f32x4 fa = __builtin_bit_cast(f32x4, a), fb = __builtin_bit_cast(f32x4, b);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[i], fb[i], acc, 0, 0, 0);
-  } else {
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0,
-                                                  0, 0);
+constexpr int parts() {
+  return sizeof(T) == 4 ? 3 : 1;
+}
+template <typename T>
+struct Operand {
+  u32x4 p[parts<T>()];  // eight values of the summed axis, each part
+};
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {  // to nearest, ties to even
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+// Two values in three parts.  GUARD: an infinity (and what rounds to it) is its third
+// part alone, which meets no part of the other operand but the first: infinity times
+// that is what the product is, where infinity times a second part of zero would be NaN.
+template <bool GUARD>
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t (&o)[3]) {
+  o[0] = pack_bf16(a, b);
+  float ha = __uint_as_float(o[0] << 16), hb = __uint_as_float(o[0] & 0xffff0000u);
+  float ra = a - ha, rb = b - hb;
+  bool ia = false, ib = false;
+  if constexpr (GUARD) {
+    ia = fabsf(ha) == INFINITY;
+    ib = fabsf(hb) == INFINITY;
+    o[0] = (ia ? 0u : o[0] & 0xffffu) | (ib ? 0u : o[0] & 0xffff0000u);
+    ra = ia ? 0.0f : ra;
+    rb = ib ? 0.0f : rb;
   }
+  o[1] = pack_bf16(ra, rb);
+  ra -= __uint_as_float(o[1] << 16);
+  rb -= __uint_as_float(o[1] & 0xffff0000u);
+  if constexpr (GUARD) {
+    ra = ia ? ha : ra;
+    rb = ib ? hb : rb;
+  }
+  o[2] = pack_bf16(ra, rb);
+}
+__device__ __forceinline__ f32x16 mfma16(const u32x4& a, const u32x4& b, const f32x16& acc) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0,
+                                                 0, 0);
 }
 
-// A row tile in LDS: rows of DP elements, 16 bytes of padding behind each (the
-// lanes of a product's operand read take the same columns of 32 rows: an odd
-// stride in units of 16 bytes spreads them over the banks).
-template <typename T, int DP>
-constexpr int tile_stride() {
-  return DP * int(sizeof(T)) + 16;
-}
-
-// The operand of columns 32 c .. 32 c + 31 (bytes) of row `row` of a tile.
-template <typename T, int DP>
-__device__ __forceinline__ u32x4 tile_chunk(const char* tile, int row, int c, int hi) {
-  return *reinterpret_cast<const u32x4*>(tile + row * tile_stride<T, DP>() + 32 * c + 16 * hi);
-}
-
-// acc[d, column] += sum over the 32 rows of a tile of tile[row][32 dt + d] p[row, column],
-// p in the layout of a result (fp32; rounded to the tile's type where that is
-// bf16: half a unit in 2^-8 of each probability or score gradient, as the
-// operands' own rounding).
-template <typename T, int DP>
-__device__ __forceinline__ void mma_transposed(const char* tile, int dt, const f32x16& p, int lane, f32x16& acc) {
-  constexpr int S = tile_stride<T, DP>();
-  const int hi = lane >> 5;
+// acc += A B over 16 values of the summed axis, of which the lane holds its half's
+// eight: A's of row lane & 31, B's of column lane & 31.
+template <typename T>
+__device__ __forceinline__ void mma(const Operand<T>& a, const Operand<T>& b, f32x16& acc) {
   if constexpr (sizeof(T) == 4) {
-    const char* base = tile + 4 * hi * S + (32 * dt + (lane & 31)) * 4;
+    acc = mfma16(a.p[0], b.p[2], acc);  // the small ones first
+    acc = mfma16(a.p[2], b.p[0], acc);
+    acc = mfma16(a.p[1], b.p[1], acc);
+    acc = mfma16(a.p[0], b.p[1], acc);
+    acc = mfma16(a.p[1], b.p[0], acc);
+  }
+  acc = mfma16(a.p[0], b.p[0], acc);
+}
+
+// A tile of rows in LDS: a plane for each part, rows of DP bf16 values, 16 bytes of
+// padding behind each (the lanes of an operand's read take the same columns of 32 rows:
+// an odd stride in units of 16 bytes spreads them over the banks).
+template <int DP>
+constexpr int row_bytes() {
+  return DP * 2 + 16;
+}
+template <typename T, int DP, int ROWS>
+constexpr int tile_bytes() {
+  return parts<T>() * ROWS * row_bytes<DP>();
+}
+
+// The operand of columns 16 c .. 16 c + 15 of row `row` of a tile of ROWS rows.
+template <typename T, int DP, int ROWS>
+__device__ __forceinline__ Operand<T> tile_operand(const char* tile, int row, int c, int hi) {
+  Operand<T> o;
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(base + tile_row(r, 0) * S), p[r], acc,
-                                                 0, 0, 0);
-  } else {
-    // 16 lanes read a block of 4 rows x 16 columns, 8 bytes each, and each
-    // receives the 4 rows of its own column
-    const char* base = tile + (4 * hi + ((lane & 15) >> 2)) * S + (32 * dt + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
-    typedef __attribute__((address_space(3))) s16x4* lds4;
+  for (int p = 0; p < parts<T>(); ++p)
+    o.p[p] = *reinterpret_cast<const u32x4*>(tile + (p * ROWS + row) * row_bytes<DP>() + 32 * c + 16 * hi);
+  return o;
+}
+
+// A result as the N-side operand of the next product, summed over its 32 rows: 16
+// values a lane, in bf16 one rounding of 2^-8 at most of each probability or score
+// gradient (as the inputs' own), in fp32 none.
+template <typename T>
+struct Columns {
+  Operand<T> s[2];
+  __device__ __forceinline__ explicit Columns(const f32x16& v) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(base + 16 * s * S));
-      const s16x4 up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(base + (16 * s + 8) * S));
-      bf16x8 a, b;
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        a[i] = __builtin_bit_cast(__bf16, short(lo[i]));
-        a[4 + i] = __builtin_bit_cast(__bf16, short(up[i]));
+      for (int j = 0; j < 4; ++j) {
+        const float x = v[8 * i + 2 * j], y = v[8 * i + 2 * j + 1];
+        if constexpr (sizeof(T) == 4) {
+          uint32_t o[3];
+          split_pair<false>(x, y, o);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) s[i].p[p][j] = o[p];
+        } else {
+          s[i].p[0][j] = pack_bf16(x, y);
+        }
       }
+  }
+};
+
+// acc[d, column] += sum over rows r0 .. r0 + 31 of a tile of tile[row][32 dt + d] v[row, column].
+template <typename T, int DP, int ROWS>
+__device__ __forceinline__ void mma_transposed(const char* tile, int r0, int dt, const Columns<T>& v, int lane,
+                                               f32x16& acc) {
+  constexpr int S = row_bytes<DP>();
+  // 16 lanes read a block of 4 rows x 16 columns, 8 bytes each, and each receives
+  // the 4 rows of its own column
+  const char* base = tile + (r0 + 4 * (lane >> 5) + ((lane & 15) >> 2)) * S +
+                     (32 * dt + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+  typedef __attribute__((address_space(3))) s16x4* lds4;
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) b[i] = static_cast<__bf16>(p[8 * s + i]);
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
+  for (int s = 0; s < 2; ++s) {
+    Operand<T> a;
+#pragma unroll
+    for (int p = 0; p < parts<T>(); ++p) {
+      const char* at = base + (p * ROWS + 16 * s) * S;
+      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at)));
+      const u32x2 up = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * S)));
+      a.p[p] = u32x4{lo[0], lo[1], up[0], up[1]};
     }
+    mma<T>(a, v.s[s], acc);
   }
 }
 
@@ -142,6 +211,58 @@ __device__ __forceinline__ u32x4 load16(const T* row, int col, int d, bool vec) 
   return z;
 }
 
+// A lane's row as N-side operands, DP / 16 of them.  RAW: fp32 values kept as they
+// are and split at each use, where the parts of them all would not fit the registers.
+template <typename T, int DP, bool RAW>
+struct RowOperands {
+  static constexpr int NC = DP / 16;
+  Operand<T> o[RAW ? 1 : NC];
+  u32x4 raw[RAW ? NC : 1][2];
+  __device__ __forceinline__ static Operand<T> split(const u32x4& a, const u32x4& b) {
+    Operand<T> r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const u32x4& v = j < 2 ? a : b;
+      uint32_t q[3];
+      split_pair<true>(__uint_as_float(v[2 * (j & 1)]), __uint_as_float(v[2 * (j & 1) + 1]), q);
+#pragma unroll
+      for (int p = 0; p < parts<T>(); ++p) r.p[p][j] = q[p];
+    }
+    return r;
+  }
+  __device__ __forceinline__ void load(const T* row, int hi, int d, bool vec) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      if constexpr (sizeof(T) == 2) {
+        o[c].p[0] = load16<T>(row, 2 * c + hi, d, vec);
+      } else {
+        const u32x4 a = load16<T>(row, 4 * c + 2 * hi, d, vec), b = load16<T>(row, 4 * c + 2 * hi + 1, d, vec);
+        if constexpr (RAW)
+          raw[c][0] = a, raw[c][1] = b;
+        else
+          o[c] = split(a, b);
+      }
+    }
+  }
+  __device__ __forceinline__ void negate() {
+    if constexpr (RAW) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) raw[c][0] ^= 0x80000000u, raw[c][1] ^= 0x80000000u;
+    } else {
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int p = 0; p < parts<T>(); ++p) o[c].p[p] ^= 0x80008000u;
+    }
+  }
+  __device__ __forceinline__ Operand<T> operator()(int c) const {
+    if constexpr (RAW)
+      return split(raw[c][0], raw[c][1]);
+    else
+      return o[c];
+  }
+};
+
 // ROWS rows from memory to an LDS tile by NT threads: fetch() issues the loads,
 // commit() writes what came.  row(r): pointer to tile row r, null where there is none.
 template <typename T, int DP, int ROWS, int NT>
@@ -159,11 +280,22 @@ struct Stage {
     }
   }
   __device__ __forceinline__ void commit(char* tile) const {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
       const int id = int(threadIdx.x) + i * NT;
       if (ROWS * CPR % NT != 0 && id >= ROWS * CPR) break;
-      *reinterpret_cast<u32x4*>(tile + (id / CPR) * tile_stride<T, DP>() + 16 * (id % CPR)) = reg[i];
+      char* const at = tile + (id / CPR) * row_bytes<DP>();
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<u32x4*>(at + 16 * (id % CPR)) = reg[i];
+      } else {
+        uint32_t a[3], b[3];
+        split_pair<true>(__uint_as_float(reg[i][0]), __uint_as_float(reg[i][1]), a);
+        split_pair<true>(__uint_as_float(reg[i][2]), __uint_as_float(reg[i][3]), b);
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+          *reinterpret_cast<u32x2*>(at + p * ROWS * row_bytes<DP>() + 8 * (id % CPR)) = u32x2{a[p], b[p]};
+      }
     }
   }
 };
@@ -308,6 +440,11 @@ struct Drop {
 template <typename T, int DP>
 constexpr int waves_per_simd() {
   return DP * int(sizeof(T)) <= 256 ? 2 : 1;
+}
+// fp32 rows longer than that stay unsplit, and the next tile is not fetched ahead.
+template <typename T, int DP>
+constexpr bool long_rows() {
+  return sizeof(T) == 4 && DP > 128;
 }
 
 // Parts of a split call: part s of element (row, i), rows counted over all heads.

@@ -20,9 +20,9 @@ constexpr int NW = 4, NT = 64 * NW, BK = 32 * NW;
 // the accumulators of all of them would not fit the registers.
 template <typename T, int DP, int DO, bool DROP>
 __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void k_attn_dkv(const AttnArgs a, int64_t n_wg, int tiles) {
-  constexpr int BR = 32, NC = DP * int(sizeof(T)) / 32, NDT = DO / 32, PARTS = DP / DO;
-  __shared__ __align__(16) char tq[BR * tile_stride<T, DP>()];
-  __shared__ __align__(16) char tg[BR * tile_stride<T, DP>()];
+  constexpr int BR = 32, NC = DP / 16, NDT = DO / 32, PARTS = DP / DO;
+  __shared__ __align__(16) char tq[tile_bytes<T, DP, BR>()];
+  __shared__ __align__(16) char tg[tile_bytes<T, DP, BR>()];
   __shared__ __align__(16) float t_ref[BR], t_delta[BR];
   lds_poison(reinterpret_cast<float*>(tq), int(sizeof(tq) / 4));
   lds_poison(reinterpret_cast<float*>(tg), int(sizeof(tg) / 4));
@@ -39,16 +39,9 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void k_attn_dkv(const Att
   const int64_t j = int64_t(tile) * BK + wave * 32 + l31;
   const bool there = j < nk;
   const bool present = there && (!a.mask || a.mask[ks + j]);  // an absent key's row is not read; its gradients are zero
-  u32x4 kf[NC], vf[NC];
-  {
-    const T* k = present ? static_cast<const T*>(a.k.p) + (ks + j) * a.k.row + w.hk * a.k.head : nullptr;
-    const T* v = present ? static_cast<const T*>(a.v.p) + (ks + j) * a.v.row + w.hk * a.v.head : nullptr;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      kf[c] = load16<T>(k, 2 * c + hi, a.d, a.vec);
-      vf[c] = load16<T>(v, 2 * c + hi, a.d, a.vec);
-    }
-  }
+  RowOperands<T, DP, long_rows<T, DP>()> kf, vf;
+  kf.load(present ? static_cast<const T*>(a.k.p) + (ks + j) * a.k.row + w.hk * a.k.head : nullptr, hi, a.d, a.vec);
+  vf.load(present ? static_cast<const T*>(a.v.p) + (ks + j) * a.v.row + w.hk * a.v.head : nullptr, hi, a.d, a.vec);
   f32x16 ak[NDT], av[NDT];
 #pragma unroll
   for (int i = 0; i < NDT; ++i) ak[i] = zero16(), av[i] = zero16();
@@ -78,8 +71,10 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void k_attn_dkv(const Att
     }
   };
   int64_t r0 = w.split * per * BR;
-  if (r0 < r_end) fetch(r0);
+  constexpr bool AHEAD = !long_rows<T, DP>();
+  if (AHEAD && r0 < r_end) fetch(r0);
   for (; r0 < r_end; r0 += BR) {
+    if (!AHEAD) fetch(r0);
     __syncthreads();
     sq.commit(tq);
     sg.commit(tg);
@@ -88,12 +83,12 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void k_attn_dkv(const Att
       t_delta[threadIdx.x] = delta;
     }
     __syncthreads();
-    if (r0 + BR < r_end) fetch(r0 + BR);  // in flight while this tile is worked on
+    if (AHEAD && r0 + BR < r_end) fetch(r0 + BR);  // in flight while this tile is worked on
     f32x16 s = zero16(), dp = zero16();
 #pragma unroll
-    for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tq, l31, c, hi), kf[c], s);
+    for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BR>(tq, l31, c, hi), kf(c), s);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tg, l31, c, hi), vf[c], dp);
+    for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BR>(tg, l31, c, hi), vf(c), dp);
     uint32_t keep = 0xffffu;
     if constexpr (DROP) keep = drop.rows_of_key(r0, int64_t(tile) * BK + wave * 32, lane);
     f32x16 p;
@@ -122,11 +117,14 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void k_attn_dkv(const Att
       for (int r = 0; r < 16; ++r)
         if (t_ref[tile_row(r, 0) + 4 * hi] == INFINITY) p[r] = s[r] = 0.0f;
     }
+    {
+      const Columns<T> pc(p);
 #pragma unroll
-    for (int i = 0; i < NDT; ++i) {
-      mma_transposed<T, DP>(tg, part * NDT + i, p, lane, av[i]);
-      mma_transposed<T, DP>(tq, part * NDT + i, s, lane, ak[i]);
+      for (int i = 0; i < NDT; ++i) mma_transposed<T, DP, BR>(tg, 0, part * NDT + i, pc, lane, av[i]);
     }
+    const Columns<T> ds(s);
+#pragma unroll
+    for (int i = 0; i < NDT; ++i) mma_transposed<T, DP, BR>(tq, 0, part * NDT + i, ds, lane, ak[i]);
   }
   if (!there) return;
   if (!present)

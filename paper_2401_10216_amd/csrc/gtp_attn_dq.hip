@@ -30,9 +30,9 @@ __global__ __launch_bounds__(256) void k_attn_delta(const AttnArgs a) {
 // Workgroup: 128 rows of one key head (4 waves x 32), keys in tiles of 32.
 template <typename T, int DP, bool DROP>
 __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_dq(const AttnArgs a, int64_t n_wg, int tiles) {
-  constexpr int BN = 32, NC = DP * int(sizeof(T)) / 32, NDT = DP / 32;
-  __shared__ __align__(16) char tk[BN * tile_stride<T, DP>()];
-  __shared__ __align__(16) char tv[BN * tile_stride<T, DP>()];
+  constexpr int BN = 32, NC = DP / 16, NDT = DP / 32;
+  __shared__ __align__(16) char tk[tile_bytes<T, DP, BN>()];
+  __shared__ __align__(16) char tv[tile_bytes<T, DP, BN>()];
   lds_poison(reinterpret_cast<float*>(tk), int(sizeof(tk) / 4));
   lds_poison(reinterpret_cast<float*>(tv), int(sizeof(tv) / 4));
   const Work w(blockIdx.x, n_wg, tiles, a.splits, a.Hk);
@@ -46,16 +46,9 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_dq(const
   const bool there = R < rows;
   const int64_t qi = there ? qs + R / a.G : 0;
   const int h = w.hk * a.G + (there ? int(R % a.G) : 0);
-  u32x4 qf[NC], gf[NC];
-  {
-    const T* q = there ? static_cast<const T*>(a.q.p) + qi * a.q.row + h * a.q.head : nullptr;
-    const T* g = there ? static_cast<const T*>(a.dout.p) + qi * a.dout.row + h * a.dout.head : nullptr;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      qf[c] = load16<T>(q, 2 * c + hi, a.d, a.vec);
-      gf[c] = load16<T>(g, 2 * c + hi, a.d, a.vec);
-    }
-  }
+  RowOperands<T, DP, long_rows<T, DP>()> qf, gf;
+  qf.load(there ? static_cast<const T*>(a.q.p) + qi * a.q.row + h * a.q.head : nullptr, hi, a.d, a.vec);
+  gf.load(there ? static_cast<const T*>(a.dout.p) + qi * a.dout.row + h * a.dout.head : nullptr, hi, a.d, a.vec);
   // rows without a key, and rows past the end: every exponential is zero
   const float lse = there ? a.lse[qi * a.H + h] : -INFINITY;
   const float ref = lse == -INFINITY ? INFINITY : lse * kLog2e;
@@ -78,18 +71,20 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_dq(const
     sv.fetch([&](int r) { return present(j0 + r) ? vb + (j0 + r) * a.v.row : nullptr; }, a.d, a.vec);
   };
   int64_t j0 = w.split * per * BN;
-  if (j0 < j_end) fetch(j0);
+  constexpr bool AHEAD = !long_rows<T, DP>();
+  if (AHEAD && j0 < j_end) fetch(j0);
   for (; j0 < j_end; j0 += BN) {
+    if (!AHEAD) fetch(j0);
     __syncthreads();
     sk.commit(tk);
     sv.commit(tv);
     __syncthreads();
-    if (j0 + BN < j_end) fetch(j0 + BN);  // in flight while this tile is worked on
+    if (AHEAD && j0 + BN < j_end) fetch(j0 + BN);  // in flight while this tile is worked on
     f32x16 s = zero16(), dp = zero16();
 #pragma unroll
-    for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tk, l31, c, hi), qf[c], s);
+    for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BN>(tk, l31, c, hi), qf(c), s);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tv, l31, c, hi), gf[c], dp);
+    for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BN>(tv, l31, c, hi), gf(c), dp);
     uint32_t keep = 0xffffu;
     if constexpr (DROP) keep = drop.keys_of_row(R0, j0, lane);
 #pragma unroll
@@ -103,8 +98,9 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_dq(const
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = (ok >> tile_row(r, 0)) & 1u ? s[r] : 0.0f;
     }
+    const Columns<T> ds(s);
 #pragma unroll
-    for (int i = 0; i < NDT; ++i) mma_transposed<T, DP>(tk, i, s, lane, acc[i]);
+    for (int i = 0; i < NDT; ++i) mma_transposed<T, DP, BN>(tk, 0, i, ds, lane, acc[i]);
   }
   if (!there) return;
   if (a.splits > 1) {

@@ -13,9 +13,9 @@ constexpr float kSlack = 8.0f;  // probabilities stay below 2^8: far from overfl
 // Workgroup: 128 rows of one key head (4 waves x 32), keys in tiles of 32 KT.
 template <typename T, int DP, int KT, bool DROP>
 __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_fwd(const AttnArgs a, int64_t n_wg, int tiles) {
-  constexpr int BN = 32 * KT, NC = DP * int(sizeof(T)) / 32, NDT = DP / 32;
-  __shared__ __align__(16) char tk[BN * tile_stride<T, DP>()];
-  __shared__ __align__(16) char tv[BN * tile_stride<T, DP>()];
+  constexpr int BN = 32 * KT, NC = DP / 16, NDT = DP / 32;
+  __shared__ __align__(16) char tk[tile_bytes<T, DP, BN>()];
+  __shared__ __align__(16) char tv[tile_bytes<T, DP, BN>()];
   lds_poison(reinterpret_cast<float*>(tk), int(sizeof(tk) / 4));
   lds_poison(reinterpret_cast<float*>(tv), int(sizeof(tv) / 4));
   const Work w(blockIdx.x, n_wg, tiles, a.splits, a.Hk);
@@ -31,13 +31,9 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_fwd(cons
   const int h = w.hk * a.G + (there ? int(R % a.G) : 0);
   // the scores' scale is taken positive, its sign into q: their maximum is then that of the products
   const float scale2 = fabsf(a.scale2);
-  u32x4 qf[NC];
-  {
-    const T* row = there ? static_cast<const T*>(a.q.p) + qi * a.q.row + h * a.q.head : nullptr;
-    const uint32_t flip = a.scale2 < 0.0f ? (sizeof(T) == 4 ? 0x80000000u : 0x80008000u) : 0u;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) qf[c] = load16<T>(row, 2 * c + hi, a.d, a.vec) ^ flip;
-  }
+  RowOperands<T, DP, long_rows<T, DP>()> qf;
+  qf.load(there ? static_cast<const T*>(a.q.p) + qi * a.q.row + h * a.q.head : nullptr, hi, a.d, a.vec);
+  if (a.scale2 < 0.0f) qf.negate();
   f32x16 acc[NDT];
 #pragma unroll
   for (int i = 0; i < NDT; ++i) acc[i] = zero16();
@@ -60,13 +56,15 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_fwd(cons
     sv.fetch([&](int r) { return present(j0 + r) ? vb + (j0 + r) * a.v.row : nullptr; }, a.d, a.vec);
   };
   int64_t j0 = w.split * per * BN;
-  if (j0 < j_end) fetch(j0);
+  constexpr bool AHEAD = !long_rows<T, DP>();
+  if (AHEAD && j0 < j_end) fetch(j0);
   for (; j0 < j_end; j0 += BN) {
+    if (!AHEAD) fetch(j0);
     __syncthreads();
     sk.commit(tk);
     sv.commit(tv);
     __syncthreads();
-    if (j0 + BN < j_end) fetch(j0 + BN);  // in flight while this tile is worked on
+    if (AHEAD && j0 + BN < j_end) fetch(j0 + BN);  // in flight while this tile is worked on
     const bool whole = !mask && j0 + BN <= nk;
     f32x16 s[KT];
     uint32_t ok[KT];
@@ -75,7 +73,7 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_fwd(cons
     for (int t = 0; t < KT; ++t) {
       s[t] = zero16();
 #pragma unroll
-      for (int c = 0; c < NC; ++c) mma_chunk<T>(tile_chunk<T, DP>(tk, 32 * t + l31, c, hi), qf[c], s[t]);
+      for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BN>(tk, 32 * t + l31, c, hi), qf(c), s[t]);
     }
     if (!whole) {
 #pragma unroll
@@ -115,9 +113,9 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_fwd(cons
         l += s[t][r];
         if constexpr (DROP) s[t][r] = (keep >> r) & 1u ? s[t][r] : 0.0f;
       }
+      const Columns<T> p(s[t]);
 #pragma unroll
-      for (int i = 0; i < NDT; ++i)
-        mma_transposed<T, DP>(tv + 32 * t * tile_stride<T, DP>(), i, s[t], lane, acc[i]);
+      for (int i = 0; i < NDT; ++i) mma_transposed<T, DP, BN>(tv, 32 * t, i, p, lane, acc[i]);
     }
   }
   l = half_sum(l);
@@ -214,7 +212,7 @@ int parts_for(int64_t n, int64_t tiles) {
 
 template <typename T, int DP>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
-  constexpr int KT = DP * int(sizeof(T)) > 256 ? 1 : 2;
+  constexpr int KT = sizeof(T) == 4 && DP > 64 ? 1 : 2;
   const int64_t tiles = (a.max_q * a.G + BM - 1) / BM, n = tiles * a.splits * a.Hk * a.B;
   if (a.threshold)
     k_attn_fwd<T, DP, KT, true><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
