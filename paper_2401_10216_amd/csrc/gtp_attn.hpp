@@ -35,6 +35,9 @@ struct AttnArgs {
   bool bf16, vec;                // vec: every row of every tensor starts 16-byte aligned, d a multiple of 16 bytes
 };
 
+// Rows (keys in dk, dv) that a workgroup takes, a wave 32: 128, or 64 where no segment has
+// more, so that short ones do not leave half the waves idle.
+inline int rows_a_tile(int64_t most) { return most <= 64 ? 64 : 128; }
 int attn_padded(int d);  // the head length that the kernels are instantiated at, >= d
 // Parts that the keys of each row (the rows of each key) are dealt to: 1 where the
 // workgroups fill the chip without.

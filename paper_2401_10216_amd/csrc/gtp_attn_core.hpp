@@ -191,25 +191,55 @@ __device__ __forceinline__ void mma_transposed(const char* tile, int r0, int dt,
   }
 }
 
-// 16 bytes at column `col` (in units of 16 bytes) of a row of d elements;
-// null row: zeros.
+// 16 bytes of a row of d elements, column `col` in units of 16 bytes: get() issues
+// the load, always (a load under a condition would make every one wait for the one
+// before it): of the row's last 16 bytes where the column passes the row's end; fix()
+// moves what came into place and puts zeros past the end, and everywhere unless `ok`.
+// vec: the row's columns are whole and its memory 16-byte aligned (else the load is
+// of element-aligned memory).
 template <typename T>
-__device__ __forceinline__ u32x4 load16(const T* row, int col, int d, bool vec) {
-  u32x4 z = {0u, 0u, 0u, 0u};
-  constexpr int E = 16 / int(sizeof(T));
-  if (row == nullptr || col * E >= d) return z;
-  if (vec) return *reinterpret_cast<const u32x4*>(row + col * E);
-  if constexpr (sizeof(T) == 4) {
+struct Load16 {
+  static constexpr int E = 16 / int(sizeof(T));
+  __device__ __forceinline__ static u32x4 get(const T* row, int col, int d, bool vec) {
+    const int at = col * E;
+    u32x4 v;
+    if (vec) {
+      v = *reinterpret_cast<const u32x4*>(row + (at < d ? at : 0));
+    } else if (d >= E) {
+      __builtin_memcpy(&v, row + (at < d - E ? at : d - E), 16);
+    } else {  // shorter rows than one load
+      v = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (col * 4 + i < d) z[i] = __float_as_uint(row[col * 4 + i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (col * 8 + i < d) z[i >> 1] |= uint32_t(row[col * 8 + i]) << (16 * (i & 1));
+      for (int i = 0; i < E; ++i) {
+        const T e = row[i < d ? i : 0];
+        if constexpr (sizeof(T) == 4)
+          v[i] = i < d ? __builtin_bit_cast(uint32_t, e) : 0u;
+        else
+          v[i >> 1] |= (i < d ? uint32_t(e) : 0u) << (16 * (i & 1));
+      }
+    }
+    return v;
   }
-  return z;
-}
+  __device__ __forceinline__ static u32x4 fix(u32x4 v, int col, int d, bool vec, bool ok) {
+    const int past = col * E + E - d;  // elements of this column behind the row's end
+    if (!vec && d >= E && past > 0 && past < E) {
+      const int bits = past * int(sizeof(T)) * 8;  // the load began as much too early
+      uint64_t lo = uint64_t(v[1]) << 32 | v[0], up = uint64_t(v[3]) << 32 | v[2];
+      if (bits >= 64) {
+        lo = bits == 64 ? up : up >> (bits - 64);
+        up = 0;
+      } else {
+        lo = lo >> bits | up << (64 - bits);
+        up >>= bits;
+      }
+      v = u32x4{uint32_t(lo), uint32_t(lo >> 32), uint32_t(up), uint32_t(up >> 32)};
+    }
+    const bool in = ok && past < E;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = in ? v[i] : 0u;
+    return v;
+  }
+};
 
 // A lane's row as N-side operands, DP / 16 of them.  RAW: fp32 values kept as they
 // are and split at each use, where the parts of them all would not fit the registers.
@@ -230,18 +260,24 @@ struct RowOperands {
     }
     return r;
   }
-  __device__ __forceinline__ void load(const T* row, int hi, int d, bool vec) {
+  // row: a valid row also where !ok (then zeros stand for it)
+  __device__ __forceinline__ void load(const T* row, bool ok, int hi, int d, bool vec) {
+    constexpr int W = sizeof(T) == 4 ? 2 : 1;
+    u32x4 v[NC][W];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int k = 0; k < W; ++k) v[c][k] = Load16<T>::get(row, W * (2 * c + hi) + k, d, vec);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      if constexpr (sizeof(T) == 2) {
-        o[c].p[0] = load16<T>(row, 2 * c + hi, d, vec);
-      } else {
-        const u32x4 a = load16<T>(row, 4 * c + 2 * hi, d, vec), b = load16<T>(row, 4 * c + 2 * hi + 1, d, vec);
-        if constexpr (RAW)
-          raw[c][0] = a, raw[c][1] = b;
-        else
-          o[c] = split(a, b);
-      }
+#pragma unroll
+      for (int k = 0; k < W; ++k) v[c][k] = Load16<T>::fix(v[c][k], W * (2 * c + hi) + k, d, vec, ok);
+      if constexpr (sizeof(T) == 2)
+        o[c].p[0] = v[c][0];
+      else if constexpr (RAW)
+        raw[c][0] = v[c][0], raw[c][1] = v[c][1];
+      else
+        o[c] = split(v[c][0], v[c][1]);
     }
   }
   __device__ __forceinline__ void negate() {
@@ -264,34 +300,49 @@ struct RowOperands {
 };
 
 // ROWS rows from memory to an LDS tile by NT threads: fetch() issues the loads,
-// commit() writes what came.  row(r): pointer to tile row r, null where there is none.
+// commit() writes what came.  row(r, &ok): pointer to tile row r, a valid one also where
+// there is none (ok = false: zeros stand for it).
 template <typename T, int DP, int ROWS, int NT>
 struct Stage {
   static constexpr int CPR = DP * int(sizeof(T)) / 16;
   static constexpr int ITER = (ROWS * CPR + NT - 1) / NT;
+  static_assert(ITER <= 32, "a bit for each load");
   u32x4 reg[ITER];
+  uint32_t ok = 0;
   template <typename F>
   __device__ __forceinline__ void fetch(F row, int d, bool vec) {
+    ok = 0;
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
       const int id = int(threadIdx.x) + i * NT;
-      if (ROWS * CPR % NT != 0 && id >= ROWS * CPR) break;
-      reg[i] = load16<T>(row(id / CPR), id % CPR, d, vec);
+      bool there = false;
+      const T* p = row(ROWS * CPR % NT != 0 && id >= ROWS * CPR ? 0 : id / CPR, &there);
+      reg[i] = Load16<T>::get(p, id % CPR, d, vec);
+      ok |= (there ? 1u : 0u) << i;
     }
   }
-  __device__ __forceinline__ void commit(char* tile) const {
+  // whole: every row of the tile is there
+  __device__ __forceinline__ void commit(char* tile, int d, bool vec, bool whole) const {
+    if (vec && whole && d == DP)
+      write<true>(tile, d, vec);
+    else
+      write<false>(tile, d, vec);
+  }
+  template <bool PLAIN>
+  __device__ __forceinline__ void write(char* tile, int d, bool vec) const {
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
       const int id = int(threadIdx.x) + i * NT;
       if (ROWS * CPR % NT != 0 && id >= ROWS * CPR) break;
       char* const at = tile + (id / CPR) * row_bytes<DP>();
+      const u32x4 v = PLAIN ? reg[i] : Load16<T>::fix(reg[i], id % CPR, d, vec, (ok >> i) & 1u);
       if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<u32x4*>(at + 16 * (id % CPR)) = reg[i];
+        *reinterpret_cast<u32x4*>(at + 16 * (id % CPR)) = v;
       } else {
         uint32_t a[3], b[3];
-        split_pair<true>(__uint_as_float(reg[i][0]), __uint_as_float(reg[i][1]), a);
-        split_pair<true>(__uint_as_float(reg[i][2]), __uint_as_float(reg[i][3]), b);
+        split_pair<true>(__uint_as_float(v[0]), __uint_as_float(v[1]), a);
+        split_pair<true>(__uint_as_float(v[2]), __uint_as_float(v[3]), b);
 #pragma unroll
         for (int p = 0; p < 3; ++p)
           *reinterpret_cast<u32x2*>(at + p * ROWS * row_bytes<DP>() + 8 * (id % CPR)) = u32x2{a[p], b[p]};

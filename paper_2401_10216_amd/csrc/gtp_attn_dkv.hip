@@ -13,14 +13,13 @@ constexpr int dkv_waves() {
   return DP * int(sizeof(T)) <= 128 ? 2 : 1;
 }
 
-constexpr int NW = 4, NT = 64 * NW, BK = 32 * NW;
 
-// Workgroup: 128 keys of one key head (4 waves x 32), rows in tiles of 32.  Heads
+// Workgroup: 32 NW keys of one key head (a wave 32), rows in tiles of 32.  Heads
 // longer than 128 are dealt to `parts` workgroups by output elements (DO each):
 // the accumulators of all of them would not fit the registers.
-template <typename T, int DP, int DO, bool DROP>
-__global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void k_attn_dkv(const AttnArgs a, int64_t n_wg, int tiles) {
-  constexpr int BR = 32, NC = DP / 16, NDT = DO / 32, PARTS = DP / DO;
+template <typename T, int DP, int DO, bool DROP, int NW>
+__global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(const AttnArgs a, int64_t n_wg, int tiles) {
+  constexpr int NT = 64 * NW, BK = 32 * NW, BR = 32, NC = DP / 16, NDT = DO / 32, PARTS = DP / DO;
   __shared__ __align__(16) char tq[tile_bytes<T, DP, BR>()];
   __shared__ __align__(16) char tg[tile_bytes<T, DP, BR>()];
   __shared__ __align__(16) float t_ref[BR], t_delta[BR];
@@ -40,8 +39,9 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void k_attn_dkv(const Att
   const bool there = j < nk;
   const bool present = there && (!a.mask || a.mask[ks + j]);  // an absent key's row is not read; its gradients are zero
   RowOperands<T, DP, long_rows<T, DP>()> kf, vf;
-  kf.load(present ? static_cast<const T*>(a.k.p) + (ks + j) * a.k.row + w.hk * a.k.head : nullptr, hi, a.d, a.vec);
-  vf.load(present ? static_cast<const T*>(a.v.p) + (ks + j) * a.v.row + w.hk * a.v.head : nullptr, hi, a.d, a.vec);
+  const int64_t jc = ks + (there ? j : nk - 1);
+  kf.load(static_cast<const T*>(a.k.p) + jc * a.k.row + w.hk * a.k.head, present, hi, a.d, a.vec);
+  vf.load(static_cast<const T*>(a.v.p) + jc * a.v.row + w.hk * a.v.head, present, hi, a.d, a.vec);
   f32x16 ak[NDT], av[NDT];
 #pragma unroll
   for (int i = 0; i < NDT; ++i) ak[i] = zero16(), av[i] = zero16();
@@ -53,14 +53,14 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void k_attn_dkv(const Att
   Stage<T, DP, BR, NT> sq, sg;
   float ref = INFINITY, delta = 0.0f;
   auto fetch = [&](int64_t r0) {
-    auto row = [&](const AttnRows& t, int r) -> const T* {
-      const int64_t R = r0 + r;
-      if (R >= rows) return nullptr;
+    auto row = [&](const AttnRows& t, int r, bool* ok) {
+      *ok = r0 + r < rows;
+      const int64_t R = *ok ? r0 + r : r0;
       const int64_t i = a.G == 1 ? R : R / a.G, g = a.G == 1 ? 0 : R % a.G;
       return static_cast<const T*>(t.p) + (qs + i) * t.row + (w.hk * a.G + g) * t.head;
     };
-    sq.fetch([&](int r) { return row(a.q, r); }, a.d, a.vec);
-    sg.fetch([&](int r) { return row(a.dout, r); }, a.d, a.vec);
+    sq.fetch([&](int r, bool* ok) { return row(a.q, r, ok); }, a.d, a.vec);
+    sg.fetch([&](int r, bool* ok) { return row(a.dout, r, ok); }, a.d, a.vec);
     ref = INFINITY;
     delta = 0.0f;
     if (threadIdx.x < BR && r0 + threadIdx.x < rows) {
@@ -76,8 +76,9 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void k_attn_dkv(const Att
   for (; r0 < r_end; r0 += BR) {
     if (!AHEAD) fetch(r0);
     __syncthreads();
-    sq.commit(tq);
-    sg.commit(tg);
+    const bool whole = r0 + BR <= rows;
+    sq.commit(tq, a.d, a.vec, whole);
+    sg.commit(tg, a.d, a.vec, whole);
     if (threadIdx.x < BR) {
       t_ref[threadIdx.x] = ref;
       t_delta[threadIdx.x] = delta;
@@ -145,14 +146,22 @@ __global__ __launch_bounds__(NT, (dkv_waves<T, DP>())) void k_attn_dkv(const Att
                      DROP ? a.keep : 1.0f, part * DO, a.d, hi, a.vec);
 }
 
+template <typename T, int DP, bool DROP>
+void launch_tiles(const AttnArgs& a, hipStream_t s) {
+  constexpr int DO = DP > 128 ? DP / 2 : DP;
+  const int64_t BK = rows_a_tile(a.max_k), tiles = (a.max_k + BK - 1) / BK, n = tiles * (DP / DO) * a.splits * a.Hk * a.B;
+  if (BK == 64)
+    k_attn_dkv<T, DP, DO, DROP, 2><<<uint32_t(n), 128, 0, s>>>(a, n, int(tiles));
+  else
+    k_attn_dkv<T, DP, DO, DROP, 4><<<uint32_t(n), 256, 0, s>>>(a, n, int(tiles));
+}
+
 template <typename T, int DP>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
-  constexpr int DO = DP > 128 ? DP / 2 : DP;
-  const int64_t tiles = (a.max_k + BK - 1) / BK, n = tiles * (DP / DO) * a.splits * a.Hk * a.B;
   if (a.threshold)
-    k_attn_dkv<T, DP, DO, true><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
+    launch_tiles<T, DP, true>(a, s);
   else
-    k_attn_dkv<T, DP, DO, false><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
+    launch_tiles<T, DP, false>(a, s);
   return hipGetLastError();
 }
 

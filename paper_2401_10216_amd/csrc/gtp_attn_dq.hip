@@ -8,7 +8,6 @@
 namespace gtp {
 namespace {
 
-constexpr int NW = 4, NT = 64 * NW, BM = 32 * NW;
 
 // delta[t, h] = sum_i dout[t, h, i] o[t, h, i]: 16 lanes a row.
 template <typename T>
@@ -27,10 +26,10 @@ __global__ __launch_bounds__(256) void k_attn_delta(const AttnArgs a) {
   if (id < n && i0 == 0) a.delta[id] = s;
 }
 
-// Workgroup: 128 rows of one key head (4 waves x 32), keys in tiles of 32.
-template <typename T, int DP, bool DROP>
-__global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_dq(const AttnArgs a, int64_t n_wg, int tiles) {
-  constexpr int BN = 32, NC = DP / 16, NDT = DP / 32;
+// Workgroup: 32 NW rows of one key head (a wave 32), keys in tiles of 32.
+template <typename T, int DP, bool DROP, int NW>
+__global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(const AttnArgs a, int64_t n_wg, int tiles) {
+  constexpr int NT = 64 * NW, BM = 32 * NW, BN = 32, NC = DP / 16, NDT = DP / 32;
   __shared__ __align__(16) char tk[tile_bytes<T, DP, BN>()];
   __shared__ __align__(16) char tv[tile_bytes<T, DP, BN>()];
   lds_poison(reinterpret_cast<float*>(tk), int(sizeof(tk) / 4));
@@ -44,11 +43,12 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_dq(const
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l31 = lane & 31, hi = lane >> 5;
   const int64_t R0 = int64_t(w.tile) * BM + wave * 32, R = R0 + l31;
   const bool there = R < rows;
-  const int64_t qi = there ? qs + R / a.G : 0;
-  const int h = w.hk * a.G + (there ? int(R % a.G) : 0);
+  const int64_t Rc = there ? R : rows - 1;  // a row past the end reads the last one and counts nothing
+  const int64_t qi = qs + Rc / a.G;
+  const int h = w.hk * a.G + int(Rc % a.G);
   RowOperands<T, DP, long_rows<T, DP>()> qf, gf;
-  qf.load(there ? static_cast<const T*>(a.q.p) + qi * a.q.row + h * a.q.head : nullptr, hi, a.d, a.vec);
-  gf.load(there ? static_cast<const T*>(a.dout.p) + qi * a.dout.row + h * a.dout.head : nullptr, hi, a.d, a.vec);
+  qf.load(static_cast<const T*>(a.q.p) + qi * a.q.row + h * a.q.head, there, hi, a.d, a.vec);
+  gf.load(static_cast<const T*>(a.dout.p) + qi * a.dout.row + h * a.dout.head, there, hi, a.d, a.vec);
   // rows without a key, and rows past the end: every exponential is zero
   const float lse = there ? a.lse[qi * a.H + h] : -INFINITY;
   const float ref = lse == -INFINITY ? INFINITY : lse * kLog2e;
@@ -67,8 +67,12 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_dq(const
   Stage<T, DP, BN, NT> sk, sv;
   auto present = [&](int64_t j) { return j < nk && (!mask || mask[j]); };
   auto fetch = [&](int64_t j0) {
-    sk.fetch([&](int r) { return present(j0 + r) ? kb + (j0 + r) * a.k.row : nullptr; }, a.d, a.vec);
-    sv.fetch([&](int r) { return present(j0 + r) ? vb + (j0 + r) * a.v.row : nullptr; }, a.d, a.vec);
+    auto row = [&](const T* base, int64_t stride, int r, bool* ok) {
+      *ok = present(j0 + r);
+      return base + (j0 + r < nk ? j0 + r : j0) * stride;
+    };
+    sk.fetch([&](int r, bool* ok) { return row(kb, a.k.row, r, ok); }, a.d, a.vec);
+    sv.fetch([&](int r, bool* ok) { return row(vb, a.v.row, r, ok); }, a.d, a.vec);
   };
   int64_t j0 = w.split * per * BN;
   constexpr bool AHEAD = !long_rows<T, DP>();
@@ -76,8 +80,9 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_dq(const
   for (; j0 < j_end; j0 += BN) {
     if (!AHEAD) fetch(j0);
     __syncthreads();
-    sk.commit(tk);
-    sv.commit(tv);
+    const bool whole = !mask && j0 + BN <= nk;
+    sk.commit(tk, a.d, a.vec, whole);
+    sv.commit(tv, a.d, a.vec, whole);
     __syncthreads();
     if (AHEAD && j0 + BN < j_end) fetch(j0 + BN);  // in flight while this tile is worked on
     f32x16 s = zero16(), dp = zero16();
@@ -93,7 +98,7 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_dq(const
       const float g = DROP ? ((keep >> r) & 1u ? dp[r] * a.keep : 0.0f) : dp[r];
       s[r] = p * (g - delta);
     }
-    if (mask || j0 + BN > nk) {
+    if (!whole) {
       const uint32_t ok = uint32_t(__ballot(present(j0 + l31))) >> (4 * hi);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = (ok >> tile_row(r, 0)) & 1u ? s[r] : 0.0f;
@@ -112,13 +117,21 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_dq(const
                    hi, a.vec);
 }
 
+template <typename T, int DP, bool DROP>
+void launch_tiles(const AttnArgs& a, hipStream_t s) {
+  const int64_t BM = rows_a_tile(a.max_q * a.G), tiles = (a.max_q * a.G + BM - 1) / BM, n = tiles * a.splits * a.Hk * a.B;
+  if (BM == 64)
+    k_attn_dq<T, DP, DROP, 2><<<uint32_t(n), 128, 0, s>>>(a, n, int(tiles));
+  else
+    k_attn_dq<T, DP, DROP, 4><<<uint32_t(n), 256, 0, s>>>(a, n, int(tiles));
+}
+
 template <typename T, int DP>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
-  const int64_t tiles = (a.max_q * a.G + BM - 1) / BM, n = tiles * a.splits * a.Hk * a.B;
   if (a.threshold)
-    k_attn_dq<T, DP, true><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
+    launch_tiles<T, DP, true>(a, s);
   else
-    k_attn_dq<T, DP, false><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
+    launch_tiles<T, DP, false>(a, s);
   return hipGetLastError();
 }
 

@@ -2,18 +2,19 @@
 // row's segment, in one pass over the keys with the running maximum and sum of
 // each row, and lse = log of the row's sum (the backward pass makes the
 // probabilities again from it).
+#include <cmath>
+
 #include "gtp_attn_core.hpp"
 
 namespace gtp {
 namespace {
 
-constexpr int NW = 4, NT = 64 * NW, BM = 32 * NW;
 constexpr float kSlack = 8.0f;  // probabilities stay below 2^8: far from overflow in fp32 and bf16, and as exact
 
-// Workgroup: 128 rows of one key head (4 waves x 32), keys in tiles of 32 KT.
-template <typename T, int DP, int KT, bool DROP>
-__global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_fwd(const AttnArgs a, int64_t n_wg, int tiles) {
-  constexpr int BN = 32 * KT, NC = DP / 16, NDT = DP / 32;
+// Workgroup: 32 NW rows of one key head (a wave 32), keys in tiles of 32 KT.
+template <typename T, int DP, int KT, bool DROP, int NW>
+__global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_fwd(const AttnArgs a, int64_t n_wg, int tiles) {
+  constexpr int NT = 64 * NW, BM = 32 * NW, BN = 32 * KT, NC = DP / 16, NDT = DP / 32;
   __shared__ __align__(16) char tk[tile_bytes<T, DP, BN>()];
   __shared__ __align__(16) char tv[tile_bytes<T, DP, BN>()];
   lds_poison(reinterpret_cast<float*>(tk), int(sizeof(tk) / 4));
@@ -27,12 +28,13 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_fwd(cons
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l31 = lane & 31, hi = lane >> 5;
   const int64_t R0 = int64_t(w.tile) * BM + wave * 32, R = R0 + l31;
   const bool there = R < rows;
-  const int64_t qi = there ? qs + R / a.G : 0;
-  const int h = w.hk * a.G + (there ? int(R % a.G) : 0);
+  const int64_t Rc = there ? R : rows - 1;  // a row past the end reads the last one and counts nothing
+  const int64_t qi = qs + Rc / a.G;
+  const int h = w.hk * a.G + int(Rc % a.G);
   // the scores' scale is taken positive, its sign into q: their maximum is then that of the products
   const float scale2 = fabsf(a.scale2);
   RowOperands<T, DP, long_rows<T, DP>()> qf;
-  qf.load(there ? static_cast<const T*>(a.q.p) + qi * a.q.row + h * a.q.head : nullptr, hi, a.d, a.vec);
+  qf.load(static_cast<const T*>(a.q.p) + qi * a.q.row + h * a.q.head, there, hi, a.d, a.vec);
   if (a.scale2 < 0.0f) qf.negate();
   f32x16 acc[NDT];
 #pragma unroll
@@ -52,8 +54,12 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_fwd(cons
   // absent keys' rows are not read: zeros stand for them
   auto present = [&](int64_t j) { return j < nk && (!mask || mask[j]); };
   auto fetch = [&](int64_t j0) {
-    sk.fetch([&](int r) { return present(j0 + r) ? kb + (j0 + r) * a.k.row : nullptr; }, a.d, a.vec);
-    sv.fetch([&](int r) { return present(j0 + r) ? vb + (j0 + r) * a.v.row : nullptr; }, a.d, a.vec);
+    auto row = [&](const T* base, int64_t stride, int r, bool* ok) {
+      *ok = present(j0 + r);
+      return base + (j0 + r < nk ? j0 + r : j0) * stride;
+    };
+    sk.fetch([&](int r, bool* ok) { return row(kb, a.k.row, r, ok); }, a.d, a.vec);
+    sv.fetch([&](int r, bool* ok) { return row(vb, a.v.row, r, ok); }, a.d, a.vec);
   };
   int64_t j0 = w.split * per * BN;
   constexpr bool AHEAD = !long_rows<T, DP>();
@@ -61,11 +67,11 @@ __global__ __launch_bounds__(NT, (waves_per_simd<T, DP>())) void k_attn_fwd(cons
   for (; j0 < j_end; j0 += BN) {
     if (!AHEAD) fetch(j0);
     __syncthreads();
-    sk.commit(tk);
-    sv.commit(tv);
+    const bool whole = !mask && j0 + BN <= nk;
+    sk.commit(tk, a.d, a.vec, whole);
+    sv.commit(tv, a.d, a.vec, whole);
     __syncthreads();
     if (AHEAD && j0 + BN < j_end) fetch(j0 + BN);  // in flight while this tile is worked on
-    const bool whole = !mask && j0 + BN <= nk;
     f32x16 s[KT];
     uint32_t ok[KT];
     float top = -INFINITY;
@@ -158,11 +164,17 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a) {
   T* const out = static_cast<T*>(const_cast<void*>(a.out.p)) + t * a.out.row + h * a.out.head;
   for (int c0 = 0; c0 < a.d; c0 += 64) {
     const int c = c0 + lane;
+    const float* const in = a.part + row * a.d + (c < a.d ? c : 0);
     float v = 0.0f;
-    for (int s = 0; s < a.splits; ++s) {
-      const float ws = __shfl(weight, s);
-      const float p = c < a.d ? a.part[(int64_t(s) * all + row) * a.d + c] : 0.0f;
-      v = ws == 0.0f ? v : fmaf(ws, p, v);
+    for (int s0 = 0; s0 < a.splits; s0 += 8) {  // eight parts' loads at a time
+      float p[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) p[k] = in[int64_t(s0 + k < a.splits ? s0 + k : 0) * all * a.d];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float ws = __shfl(weight, (s0 + k) & 63);  // 0 past the last part
+        v = s0 + k >= a.splits || ws == 0.0f ? v : fmaf(ws, p[k], v);
+      }
     }
     if (c < a.d) {
       if constexpr (sizeof(T) == 4) {
@@ -199,25 +211,38 @@ __global__ __launch_bounds__(256) void k_attn_sum(const float* __restrict__ part
   }
 }
 
-constexpr int64_t kFill = 768;  // workgroups, three a CU
+// Parts for n workgroups whose loops take `tiles` tiles, at `per_cu` of them a CU at a
+// time: as few as keep the CUs nine tenths busy to the end of the last round (n a
+// little above a round leaves most of them idle in the second), two tiles each at least.
+int parts_for(int64_t n, int64_t tiles, int per_cu) {
+  const int64_t slots = 256 * per_cu;
+  if (n <= 0 || n >= 8 * slots) return 1;
+  int64_t best = 1;
+  double use = 0.0;
+  for (int64_t s = 1; s <= 64 && (s == 1 || s <= tiles / 2); ++s) {
+    const double rounds = double(n * s) / double(slots), u = rounds / std::ceil(rounds);
+    if (u > use + 0.02) use = u, best = s;
+    if (use >= 0.9) break;
+  }
+  return int(best);
+}
 
-// Parts for n workgroups whose loops take `tiles` tiles: enough for kFill
-// workgroups, two tiles each at least.
-int parts_for(int64_t n, int64_t tiles) {
-  if (n <= 0 || n >= kFill / 2) return 1;
-  int64_t s = (kFill + n - 1) / n;
-  if (s > tiles / 2) s = tiles / 2;
-  return s < 1 ? 1 : s > 64 ? 64 : int(s);
+template <typename T, int DP, bool DROP>
+void launch_tiles(const AttnArgs& a, hipStream_t s) {
+  constexpr int KT = sizeof(T) == 4 && DP > 64 ? 1 : 2;
+  const int64_t BM = rows_a_tile(a.max_q * a.G), tiles = (a.max_q * a.G + BM - 1) / BM, n = tiles * a.splits * a.Hk * a.B;
+  if (BM == 64)
+    k_attn_fwd<T, DP, KT, DROP, 2><<<uint32_t(n), 128, 0, s>>>(a, n, int(tiles));
+  else
+    k_attn_fwd<T, DP, KT, DROP, 4><<<uint32_t(n), 256, 0, s>>>(a, n, int(tiles));
 }
 
 template <typename T, int DP>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
-  constexpr int KT = sizeof(T) == 4 && DP > 64 ? 1 : 2;
-  const int64_t tiles = (a.max_q * a.G + BM - 1) / BM, n = tiles * a.splits * a.Hk * a.B;
   if (a.threshold)
-    k_attn_fwd<T, DP, KT, true><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
+    launch_tiles<T, DP, true>(a, s);
   else
-    k_attn_fwd<T, DP, KT, false><<<uint32_t(n), NT, 0, s>>>(a, n, int(tiles));
+    launch_tiles<T, DP, false>(a, s);
   if (a.splits > 1) {
     const int64_t rows = (a.max_q * a.H + 3) / 4 * a.B;
     k_attn_join<T><<<uint32_t(rows), 256, 0, s>>>(a);
@@ -229,11 +254,22 @@ hipError_t launch(const AttnArgs& a, hipStream_t s) {
 
 int attn_padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256; }
 
+// Workgroups that a CU holds, by the registers that the kernels are cut for.
+namespace {
+int wg_a_cu(const AttnArgs& a, bool keys) {
+  const int bytes = attn_padded(a.d) * (a.bf16 ? 2 : 4);
+  return bytes <= (keys ? 128 : 256) ? 2 : 1;
+}
+}  // namespace
+
 int attn_row_splits(const AttnArgs& a) {
-  return parts_for((a.max_q * a.G + BM - 1) / BM * a.Hk * a.B, (a.max_k + 63) / 64);
+  const int BM = rows_a_tile(a.max_q * a.G);
+  return parts_for((a.max_q * a.G + BM - 1) / BM * a.Hk * a.B, (a.max_k + 63) / 64, wg_a_cu(a, false));
 }
 int attn_key_splits(const AttnArgs& a) {
-  return parts_for((a.max_k + 127) / 128 * a.Hk * a.B, (a.max_q * a.G + 63) / 64);
+  const int BK = rows_a_tile(a.max_k);
+  return parts_for((a.max_k + BK - 1) / BK * (attn_padded(a.d) > 128 ? 2 : 1) * a.Hk * a.B, (a.max_q * a.G + 63) / 64,
+                   wg_a_cu(a, true));
 }
 
 hipError_t launch_attn_sum(const AttnArgs& a, const float* part, int splits, bool keys, const AttnRows& out,
