@@ -362,6 +362,25 @@ __device__ __forceinline__ void segment(const int64_t* off, int64_t b, int64_t m
   n = e - s < most ? e - s : most;
 }
 
+// Row R = i G + g of a key head's rows: i, and g in *g.  (64-bit divisions in the tile
+// loop took longer than its products; R < 2^31 by the launch's limits.)
+struct Group {
+  uint32_t G, inv;
+  __device__ __forceinline__ explicit Group(int g) : G(uint32_t(g)), inv(g > 1 ? 0xffffffffu / uint32_t(g) : 0) {}
+  __device__ __forceinline__ int64_t row(int64_t R, int* g) const {
+    if (G == 1) {
+      *g = 0;
+      return R;
+    }
+    uint32_t q = __umulhi(uint32_t(R), inv);  // at most two too few
+    uint32_t r = uint32_t(R) - q * G;
+    if (r >= G) ++q, r -= G;
+    if (r >= G) ++q, r -= G;
+    *g = int(r);
+    return int64_t(q);
+  }
+};
+
 // Element type of the tensors in memory.
 template <typename T>
 __device__ __forceinline__ float to_f32(T v) {

@@ -10,16 +10,16 @@ namespace {
 // Keys, values and both accumulators take twice what dq's rows do.
 template <typename T, int DP>
 constexpr int dkv_waves() {
-  return DP * int(sizeof(T)) <= 128 ? 2 : 1;
+  return DP * int(sizeof(T)) <= 128 || (sizeof(T) == 2 && DP <= 128) ? 2 : 1;
 }
 
 
 // Workgroup: 32 NW keys of one key head (a wave 32), rows in tiles of 32.  Heads
 // longer than 128 are dealt to `parts` workgroups by output elements (DO each):
 // the accumulators of all of them would not fit the registers.
-template <typename T, int DP, int DO, bool DROP, int NW>
+template <typename T, int DP, int DO, int RT, bool DROP, int NW>
 __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(const AttnArgs a, int64_t n_wg, int tiles) {
-  constexpr int NT = 64 * NW, BK = 32 * NW, BR = 32, NC = DP / 16, NDT = DO / 32, PARTS = DP / DO;
+  constexpr int NT = 64 * NW, BK = 32 * NW, BR = 32 * RT, NC = DP / 16, NDT = DO / 32, PARTS = DP / DO;
   __shared__ __align__(16) char tq[tile_bytes<T, DP, BR>()];
   __shared__ __align__(16) char tg[tile_bytes<T, DP, BR>()];
   __shared__ __align__(16) float t_ref[BR], t_delta[BR];
@@ -50,13 +50,15 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
 
   const int64_t ntile = (rows + BR - 1) / BR, per = (ntile + a.splits - 1) / a.splits;
   const int64_t r_end = (w.split + 1) * per * BR < rows ? (w.split + 1) * per * BR : rows;
+  const Group group(a.G);
   Stage<T, DP, BR, NT> sq, sg;
   float ref = INFINITY, delta = 0.0f;
   auto fetch = [&](int64_t r0) {
     auto row = [&](const AttnRows& t, int r, bool* ok) {
       *ok = r0 + r < rows;
       const int64_t R = *ok ? r0 + r : r0;
-      const int64_t i = a.G == 1 ? R : R / a.G, g = a.G == 1 ? 0 : R % a.G;
+      int g;
+      const int64_t i = group.row(R, &g);
       return static_cast<const T*>(t.p) + (qs + i) * t.row + (w.hk * a.G + g) * t.head;
     };
     sq.fetch([&](int r, bool* ok) { return row(a.q, r, ok); }, a.d, a.vec);
@@ -64,14 +66,15 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
     ref = INFINITY;
     delta = 0.0f;
     if (threadIdx.x < BR && r0 + threadIdx.x < rows) {
-      const int64_t R = r0 + threadIdx.x, at = (qs + R / a.G) * a.H + w.hk * a.G + R % a.G;
+      int g;
+      const int64_t i = group.row(r0 + threadIdx.x, &g), at = (qs + i) * a.H + w.hk * a.G + g;
       const float lse = a.lse[at];
       ref = lse == -INFINITY ? INFINITY : lse * kLog2e;
       delta = a.delta[at];
     }
   };
   int64_t r0 = w.split * per * BR;
-  constexpr bool AHEAD = !long_rows<T, DP>();
+  constexpr bool AHEAD = !long_rows<T, DP>() && !(sizeof(T) == 2 && DP == 128);  // there the registers hold no more
   if (AHEAD && r0 < r_end) fetch(r0);
   for (; r0 < r_end; r0 += BR) {
     if (!AHEAD) fetch(r0);
@@ -85,47 +88,50 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
     }
     __syncthreads();
     if (AHEAD && r0 + BR < r_end) fetch(r0 + BR);  // in flight while this tile is worked on
-    f32x16 s = zero16(), dp = zero16();
 #pragma unroll
-    for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BR>(tq, l31, c, hi), kf(c), s);
+    for (int t = 0; t < RT; ++t) {
+      f32x16 s = zero16(), dp = zero16();
 #pragma unroll
-    for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BR>(tg, l31, c, hi), vf(c), dp);
-    uint32_t keep = 0xffffu;
-    if constexpr (DROP) keep = drop.rows_of_key(r0, int64_t(tile) * BK + wave * 32, lane);
-    f32x16 p;
+      for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BR>(tq, 32 * t + l31, c, hi), kf(c), s);
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const f32x4 rf = *reinterpret_cast<const f32x4*>(t_ref + 8 * g + 4 * hi);
-      const f32x4 de = *reinterpret_cast<const f32x4*>(t_delta + 8 * g + 4 * hi);
+      for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BR>(tg, 32 * t + l31, c, hi), vf(c), dp);
+      uint32_t keep = 0xffffu;
+      if constexpr (DROP) keep = drop.rows_of_key(r0 + 32 * t, int64_t(tile) * BK + wave * 32, lane);
+      f32x16 p;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = 4 * g + i;
-        const float e = pow2(fmaf(s[r], a.scale2, -rf[i]));
-        if constexpr (DROP) {
-          const bool kept = (keep >> r) & 1u;
-          p[r] = kept ? e : 0.0f;
-          s[r] = e * ((kept ? dp[r] * a.keep : 0.0f) - de[i]);
-        } else {
-          p[r] = e;
-          s[r] = e * (dp[r] - de[i]);
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 rf = *reinterpret_cast<const f32x4*>(t_ref + 32 * t + 8 * g + 4 * hi);
+        const f32x4 de = *reinterpret_cast<const f32x4*>(t_delta + 32 * t + 8 * g + 4 * hi);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 4 * g + i;
+          const float e = pow2(fmaf(s[r], a.scale2, -rf[i]));
+          if constexpr (DROP) {
+            const bool kept = (keep >> r) & 1u;
+            p[r] = kept ? e : 0.0f;
+            s[r] = e * ((kept ? dp[r] * a.keep : 0.0f) - de[i]);
+          } else {
+            p[r] = e;
+            s[r] = e * (dp[r] - de[i]);
+          }
         }
       }
-    }
-    // rows past the end and rows without a key count nothing, whatever k and v
-    // hold (a zero of theirs times an infinity would be NaN)
-    if (__any(t_ref[l31] == INFINITY)) {
+      // rows past the end and rows without a key count nothing, whatever k and v
+      // hold (a zero of theirs times an infinity would be NaN)
+      if (__any(t_ref[32 * t + l31] == INFINITY)) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (t_ref[tile_row(r, 0) + 4 * hi] == INFINITY) p[r] = s[r] = 0.0f;
-    }
-    {
-      const Columns<T> pc(p);
+        for (int r = 0; r < 16; ++r)
+          if (t_ref[32 * t + tile_row(r, 0) + 4 * hi] == INFINITY) p[r] = s[r] = 0.0f;
+      }
+      {
+        const Columns<T> pc(p);
 #pragma unroll
-      for (int i = 0; i < NDT; ++i) mma_transposed<T, DP, BR>(tg, 0, part * NDT + i, pc, lane, av[i]);
-    }
-    const Columns<T> ds(s);
+        for (int i = 0; i < NDT; ++i) mma_transposed<T, DP, BR>(tg, 32 * t, part * NDT + i, pc, lane, av[i]);
+      }
+      const Columns<T> ds(s);
 #pragma unroll
-    for (int i = 0; i < NDT; ++i) mma_transposed<T, DP, BR>(tq, 0, part * NDT + i, ds, lane, ak[i]);
+      for (int i = 0; i < NDT; ++i) mma_transposed<T, DP, BR>(tq, 32 * t, part * NDT + i, ds, lane, ak[i]);
+    }
   }
   if (!there) return;
   if (!present)
@@ -148,12 +154,12 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
 
 template <typename T, int DP, bool DROP>
 void launch_tiles(const AttnArgs& a, hipStream_t s) {
-  constexpr int DO = DP > 128 ? DP / 2 : DP;
+  constexpr int DO = DP > 128 ? DP / 2 : DP, RT = DP * int(sizeof(T)) <= 128 ? 2 : 1;
   const int64_t BK = rows_a_tile(a.max_k), tiles = (a.max_k + BK - 1) / BK, n = tiles * (DP / DO) * a.splits * a.Hk * a.B;
   if (BK == 64)
-    k_attn_dkv<T, DP, DO, DROP, 2><<<uint32_t(n), 128, 0, s>>>(a, n, int(tiles));
+    k_attn_dkv<T, DP, DO, RT, DROP, 2><<<uint32_t(n), 128, 0, s>>>(a, n, int(tiles));
   else
-    k_attn_dkv<T, DP, DO, DROP, 4><<<uint32_t(n), 256, 0, s>>>(a, n, int(tiles));
+    k_attn_dkv<T, DP, DO, RT, DROP, 4><<<uint32_t(n), 256, 0, s>>>(a, n, int(tiles));
 }
 
 template <typename T, int DP>

@@ -44,8 +44,9 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
   const int64_t R0 = int64_t(w.tile) * BM + wave * 32, R = R0 + l31;
   const bool there = R < rows;
   const int64_t Rc = there ? R : rows - 1;  // a row past the end reads the last one and counts nothing
-  const int64_t qi = qs + Rc / a.G;
-  const int h = w.hk * a.G + int(Rc % a.G);
+  int g;
+  const int64_t qi = qs + Group(a.G).row(Rc, &g);
+  const int h = w.hk * a.G + g;
   RowOperands<T, DP, long_rows<T, DP>()> qf, gf;
   qf.load(static_cast<const T*>(a.q.p) + qi * a.q.row + h * a.q.head, there, hi, a.d, a.vec);
   gf.load(static_cast<const T*>(a.dout.p) + qi * a.dout.row + h * a.dout.head, there, hi, a.d, a.vec);

@@ -29,8 +29,9 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_fwd
   const int64_t R0 = int64_t(w.tile) * BM + wave * 32, R = R0 + l31;
   const bool there = R < rows;
   const int64_t Rc = there ? R : rows - 1;  // a row past the end reads the last one and counts nothing
-  const int64_t qi = qs + Rc / a.G;
-  const int h = w.hk * a.G + int(Rc % a.G);
+  int g;
+  const int64_t qi = qs + Group(a.G).row(Rc, &g);
+  const int h = w.hk * a.G + g;
   // the scores' scale is taken positive, its sign into q: their maximum is then that of the products
   const float scale2 = fabsf(a.scale2);
   RowOperands<T, DP, long_rows<T, DP>()> qf;
@@ -258,7 +259,7 @@ int attn_padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <
 namespace {
 int wg_a_cu(const AttnArgs& a, bool keys) {
   const int bytes = attn_padded(a.d) * (a.bf16 ? 2 : 4);
-  return bytes <= (keys ? 128 : 256) ? 2 : 1;
+  return bytes <= (keys && !a.bf16 ? 128 : 256) ? 2 : 1;
 }
 }  // namespace
 
