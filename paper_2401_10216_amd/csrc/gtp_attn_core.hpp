@@ -480,13 +480,21 @@ struct Drop {
   }
   // Bit h: whether draw h of a call keeps.
   __device__ __forceinline__ uint32_t kept8(const uint32_t (&w)[4]) const {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    const uint16_t below = uint16_t(threshold - 1);  // threshold > 0 where anything is dropped
     uint32_t b = 0;
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
-      b |= ((w[h] & 0xffffu) >= threshold ? 1u : 0u) << (2 * h);
-      b |= ((w[h] >> 16) >= threshold ? 1u : 0u) << (2 * h + 1);
+      // both halves at once: draw - (threshold - 1), at least 0 and at most 1
+      const u16x2 over = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, w[h]), u16x2{below, below});
+      const uint32_t one = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(over, u16x2{1, 1}));
+      b |= ((one | one >> 15) & 3u) << (2 * h);
     }
     return b;
+  }
+  // v where bit r of keep is set, else 0.
+  __device__ __forceinline__ static float kept(float v, uint32_t keep, int r) {
+    return __uint_as_float(__float_as_uint(v) & uint32_t(__builtin_amdgcn_sbfe(int(keep), r, 1)));
   }
   // Lane q of a quad holds block q's nibbles; it gets nibble q of each block g, at bits 4 g.
   __device__ __forceinline__ static uint32_t trade(uint32_t bits, int q) {

@@ -107,9 +107,8 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
           const int r = 4 * g + i;
           const float e = pow2(fmaf(s[r], a.scale2, -rf[i]));
           if constexpr (DROP) {
-            const bool kept = (keep >> r) & 1u;
-            p[r] = kept ? e : 0.0f;
-            s[r] = e * ((kept ? dp[r] * a.keep : 0.0f) - de[i]);
+            p[r] = Drop::kept(e, keep, r);
+            s[r] = e * (Drop::kept(dp[r] * a.keep, keep, r) - de[i]);
           } else {
             p[r] = e;
             s[r] = e * (dp[r] - de[i]);

@@ -96,7 +96,7 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float p = pow2(fmaf(s[r], a.scale2, -ref));
-      const float g = DROP ? ((keep >> r) & 1u ? dp[r] * a.keep : 0.0f) : dp[r];
+      const float g = DROP ? Drop::kept(dp[r] * a.keep, keep, r) : dp[r];
       s[r] = p * (g - delta);
     }
     if (!whole) {

@@ -13,7 +13,7 @@ constexpr float kSlack = 8.0f;  // probabilities stay below 2^8: far from overfl
 
 // Workgroup: 32 NW rows of one key head (a wave 32), keys in tiles of 32 KT.
 template <typename T, int DP, int KT, bool DROP, int NW>
-__global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_fwd(const AttnArgs a, int64_t n_wg, int tiles) {
+__global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const AttnArgs a, int64_t n_wg, int tiles) {
   constexpr int NT = 64 * NW, BM = 32 * NW, BN = 32 * KT, NC = DP / 16, NDT = DP / 32;
   __shared__ __align__(16) char tk[tile_bytes<T, DP, BN>()];
   __shared__ __align__(16) char tv[tile_bytes<T, DP, BN>()];
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_fwd
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         l += s[t][r];
-        if constexpr (DROP) s[t][r] = (keep >> r) & 1u ? s[t][r] : 0.0f;
+        if constexpr (DROP) s[t][r] = Drop::kept(s[t][r], keep, r);
       }
       const Columns<T> p(s[t]);
 #pragma unroll

@@ -7,8 +7,10 @@ is not built the import of any entry point raises -- there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
+import struct
 import threading
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -41,6 +43,7 @@ _U = ctypes.c_uint
 _DP = ctypes.POINTER(ctypes.c_double)
 
 
+
 class _Rows(ctypes.Structure):
     """gtp_rows."""
     _fields_ = [("data", _P), ("row", _I64), ("head", _I64)]
@@ -52,6 +55,11 @@ class _Attn(ctypes.Structure):
                 ("max_q", _I64), ("max_k", _I64), ("q_off", _P), ("k_off", _P), ("key_mask", _P),
                 ("scale", ctypes.c_float), ("p", ctypes.c_double), ("rng", _P)]
 
+
+# The same layouts to pack a call's structs with (a Structure's fields one by one take several times as long).
+_ATTN = struct.Struct("<4i5q3Qf4xdQ")
+_ROWS = "Qqq"
+assert _ATTN.size == ctypes.sizeof(_Attn) and struct.calcsize("<" + _ROWS) == ctypes.sizeof(_Rows)
 
 _SIGS = {
     "gtp_plan_create": (_I, [ctypes.POINTER(_P), _I, _I, _I, _U]),
@@ -135,6 +143,9 @@ def _check(status: int, L=None):
 
 def _stream(stream=None):
     import torch
+    if stream is None and torch.cuda.is_initialized():
+        # the current stream's handle without a Stream object around it (several us a call)
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
     s = stream if stream is not None else torch.cuda.current_stream()
     return ctypes.c_void_p(s.cuda_stream)
 
@@ -166,13 +177,13 @@ def _want(t, name, shape, dtypes, device=None):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype not in dtypes:
         raise TypeError(f"{name} has dtype {t.dtype}; expected " + " or ".join(str(d) for d in dtypes))
-    if tuple(t.shape) != tuple(int(v) for v in shape):
+    if t.shape != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}; expected {tuple(int(v) for v in shape)}")
     if device is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}; the other operands are on {device}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _on_gpu(t, name):
@@ -489,22 +500,24 @@ class _on_stream:
 
     def __init__(self, stream):
         import torch
-        self.ctx = torch.cuda.stream(stream) if stream is not None else None
+        self.ctx = torch.cuda.stream(stream)
 
     def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
+        self.ctx.__enter__()
 
     def __exit__(self, *exc):
-        return self.ctx.__exit__(*exc) if self.ctx is not None else False
+        return self.ctx.__exit__(*exc)
 
 
-def _null():
-    return ctypes.c_void_p(None)
+_HERE = contextlib.nullcontext()
+
+
+def _allocating(stream):
+    return _HERE if stream is None else _on_stream(stream)
 
 
 def _opt(t, name, shape, dtypes, device):
-    return _null() if t is None else _want(t, name, shape, dtypes, device)
+    return None if t is None else _want(t, name, shape, dtypes, device)
 
 
 def _rng_state(rng, device):
@@ -512,13 +525,8 @@ def _rng_state(rng, device):
     return _want(rng, "rng", (2,), (torch.int64, torch.uint64), device)
 
 
-def _work(nbytes: int, device):
-    import torch
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes > 0 else None
-
-
 def _ptr(t):
-    return _null() if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def gtp_layer_norm(x, L: int, w=None, b=None, eps: float = 1e-5, y=None, mean=None, rstd=None, stream=None):
@@ -526,22 +534,25 @@ def gtp_layer_norm(x, L: int, w=None, b=None, eps: float = 1e-5, y=None, mean=No
     scaled by w[L+1, C] and, at degree 0, shifted by b[C] (fp32 or None); y has x's type, mean[N] and rstd[N, L+1]
     fp32 are what the backward reads.  y may be x."""
     import torch
+    f32 = torch.float32
     if x.dim() != 3 or x.shape[2] != nsh(L):
         raise ValueError("x must be [N, C, (L+1)^2]")
-    N, C = int(x.shape[0]), int(x.shape[1])
+    N, C, _ = x.shape
+    dev, one = x.device, (f32,)
     code = _dtype_code(x)
-    px = _want(x, "x", x.shape, _inputs())
-    pw = _opt(w, "w", (L + 1, C), _f32(), x.device)
-    pb = _opt(b, "b", (C,), _f32(), x.device)
-    with _on_stream(stream):
+    px = _want(x, "x", x.shape, (x.dtype,))
+    pw = _opt(w, "w", (L + 1, C), one, dev)
+    pb = _opt(b, "b", (C,), one, dev)
+    with _allocating(stream):
         y = torch.empty_like(x) if y is None else y
-        mean = torch.empty(N, dtype=torch.float32, device=x.device) if mean is None else mean
-        rstd = torch.empty((N, L + 1), dtype=torch.float32, device=x.device) if rstd is None else rstd
-    py = _want(y, "y", x.shape, (x.dtype,), x.device)
-    pm = _want(mean, "mean", (N,), _f32(), x.device)
-    pr = _want(rstd, "rstd", (N, L + 1), _f32(), x.device)
+        mean = torch.empty(N, dtype=f32, device=dev) if mean is None else mean
+        rstd = torch.empty((N, L + 1), dtype=f32, device=dev) if rstd is None else rstd
+    py = _want(y, "y", x.shape, (x.dtype,), dev)
+    pm = _want(mean, "mean", (N,), one, dev)
+    pr = _want(rstd, "rstd", (N, L + 1), one, dev)
     _on_gpu(x, "x")
-    _check(lib().gtp_layer_norm(L, px, code, pw, pb, eps, N, C, py, pm, pr, _stream(stream)))
+    lib_ = lib()
+    _check(lib_.gtp_layer_norm(L, px, code, pw, pb, eps, N, C, py, pm, pr, _stream(stream)), lib_)
     return y, mean, rstd
 
 
@@ -549,31 +560,34 @@ def gtp_layer_norm_backward(x, dy, L: int, mean, rstd, w=None, need=("dx", "dw",
     """Gradients of <dy, gtp_layer_norm(x, L, w, b)>: a dict with the requested keys among dx (like x), dw[L+1, C] and
     db[C] (fp32); mean, rstd as gtp_layer_norm returned them."""
     import torch
+    f32 = torch.float32
     if x.dim() != 3 or x.shape[2] != nsh(L):
         raise ValueError("x must be [N, C, (L+1)^2]")
     unknown = set(need) - {"dx", "dw", "db"}
     if unknown:
         raise ValueError(f"unknown gradients {sorted(unknown)}")
-    N, C = int(x.shape[0]), int(x.shape[1])
+    N, C, _ = x.shape
+    dev, one = x.device, (f32,)
     code = _dtype_code(x)
-    px = _want(x, "x", x.shape, _inputs())
-    pdy = _want(dy, "dy", x.shape, (x.dtype,), x.device)
-    pw = _opt(w, "w", (L + 1, C), _f32(), x.device)
-    pm = _want(mean, "mean", (N,), _f32(), x.device)
-    pr = _want(rstd, "rstd", (N, L + 1), _f32(), x.device)
+    px = _want(x, "x", x.shape, (x.dtype,))
+    pdy = _want(dy, "dy", x.shape, (x.dtype,), dev)
+    pw = _opt(w, "w", (L + 1, C), one, dev)
+    pm = _want(mean, "mean", (N,), one, dev)
+    pr = _want(rstd, "rstd", (N, L + 1), one, dev)
     _on_gpu(x, "x")
+    lib_ = lib()
+    nbytes = lib_.gtp_layer_norm_backward_work(L, code, N, C) if "dw" in need or "db" in need else 0
     out = {}
-    with _on_stream(stream):
+    with _allocating(stream):
         if "dx" in need:
             out["dx"] = torch.empty_like(x)
         if "dw" in need:
-            out["dw"] = torch.empty((L + 1, C), dtype=torch.float32, device=x.device)
+            out["dw"] = torch.empty((L + 1, C), dtype=f32, device=dev)
         if "db" in need:
-            out["db"] = torch.empty(C, dtype=torch.float32, device=x.device)
-        nbytes = lib().gtp_layer_norm_backward_work(L, code, N, C) if "dw" in need or "db" in need else 0
-        work = _work(nbytes, x.device)
-    _check(lib().gtp_layer_norm_backward(L, px, code, pw, pm, pr, pdy, N, C, _ptr(out.get("dx")), _ptr(out.get("dw")),
-                                         _ptr(out.get("db")), _ptr(work), nbytes, _stream(stream)))
+            out["db"] = torch.empty(C, dtype=f32, device=dev)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes > 0 else None
+    _check(lib_.gtp_layer_norm_backward(L, px, code, pw, pm, pr, pdy, N, C, _ptr(out.get("dx")), _ptr(out.get("dw")),
+                                        _ptr(out.get("db")), _ptr(work), nbytes, _stream(stream)), lib_)
     return out
 
 
@@ -585,16 +599,19 @@ def gtp_dropout(x, p: float, rng, res=None, y=None, stream=None):
     if x.dim() < 1:
         raise ValueError("x must have a last dimension")
     code = _dtype_code(x)
-    K = int(x.shape[-1])
+    K = x.shape[-1]
     groups = x.numel() // K if K else 0
-    px = _want(x, "x", x.shape, _inputs())
-    pres = _opt(res, "res", x.shape, (x.dtype,), x.device)
-    prng = _rng_state(rng, x.device)
-    with _on_stream(stream):
-        y = torch.empty_like(x) if y is None else y
-    py = _want(y, "y", x.shape, (x.dtype,), x.device)
+    dev, own = x.device, (x.dtype,)
+    px = _want(x, "x", x.shape, own)
+    pres = _opt(res, "res", x.shape, own, dev)
+    prng = _rng_state(rng, dev)
+    if y is None:
+        with _allocating(stream):
+            y = torch.empty_like(x)
+    py = _want(y, "y", x.shape, own, dev)
     _on_gpu(x, "x")
-    _check(lib().gtp_dropout(px, pres, code, p, prng, groups, K, py, _stream(stream)))
+    lib_ = lib()
+    _check(lib_.gtp_dropout(px, pres, code, p, prng, groups, K, py, _stream(stream)), lib_)
     return y
 
 
@@ -606,28 +623,30 @@ def _attn_rows(t, name, shape, dtype, device):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} has dtype {t.dtype}; expected {dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}; expected {tuple(shape)}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}; the other operands are on {device}")
-    if t.shape[2] > 1 and t.stride(2) != 1:
+    row, head, one = t.stride()
+    if one != 1 and shape[2] > 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
-    return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+    return t.data_ptr(), row, head
 
 
 def _attn(q, k, v, scale, q_off, k_off, max_q, max_k, key_mask, p, rng):
-    """Validated gtp_attn and the rows of q, k, v."""
+    """Validated gtp_attn and the rows of q, k, v, as their fields."""
     import torch
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q must be [Tq, H, d], k and v [Tk, Hk, d]")
     code = _dtype_code(q)
-    Tq, H, d = (int(i) for i in q.shape)
-    Tk, Hk = int(k.shape[0]), int(k.shape[1])
-    i64 = (torch.int64,)
+    Tq, H, d = q.shape
+    Tk, Hk, _ = k.shape
+    dev, dt = q.device, q.dtype
     if H < 1 or Hk < 1 or d < 1 or H % Hk:
         raise ValueError("the number of query heads must be a positive multiple of the number of key heads")
-    rows = [_attn_rows(q, "q", (Tq, H, d), q.dtype, q.device), _attn_rows(k, "k", (Tk, Hk, d), q.dtype, q.device),
-            _attn_rows(v, "v", (Tk, Hk, d), q.dtype, q.device)]
+    kshape = (Tk, Hk, d)
+    rows = (*_attn_rows(q, "q", q.shape, dt, dev), *_attn_rows(k, "k", kshape, dt, dev),
+            *_attn_rows(v, "v", kshape, dt, dev))
     B = None
     for off, name in ((q_off, "q_off"), (k_off, "k_off")):
         if off is None:
@@ -636,18 +655,29 @@ def _attn(q, k, v, scale, q_off, k_off, max_q, max_k, key_mask, p, rng):
             raise ValueError(f"{name} must be [B + 1]")
         if B is not None and off.shape[0] != B + 1:
             raise ValueError("q_off and k_off must have one length")
-        B = int(off.shape[0]) - 1
+        B = off.shape[0] - 1
     if B is None:
         # equal segments: of max_q and max_k rows, or one of all rows
         n, most = (Tq, max_q) if max_q is not None else (Tk, max_k)
         B = 1 if most is None else (n // most if most else 1)
     max_q = (Tq if q_off is not None else Tq // max(B, 1)) if max_q is None else int(max_q)
     max_k = (Tk if k_off is not None else Tk // max(B, 1)) if max_k is None else int(max_k)
-    desc = _Attn(code, H, Hk, d, B, Tq, Tk, min(max_q, Tq), min(max_k, Tk), _opt(q_off, "q_off", (B + 1,), i64, q.device),
-                 _opt(k_off, "k_off", (B + 1,), i64, q.device),
-                 _opt(key_mask, "key_mask", (Tk,), (torch.uint8, torch.bool), q.device),
-                 1.0 / d ** 0.5 if scale is None else scale, p, _null() if rng is None else _rng_state(rng, q.device))
+    i64 = (torch.int64,)
+    desc = (code, H, Hk, d, B, Tq, Tk, min(max_q, Tq), min(max_k, Tk),
+            _opt(q_off, "q_off", (B + 1,), i64, dev) or 0, _opt(k_off, "k_off", (B + 1,), i64, dev) or 0,
+            _opt(key_mask, "key_mask", (Tk,), (torch.uint8, torch.bool), dev) or 0,
+            1.0 / d ** 0.5 if scale is None else scale, p, 0 if rng is None else _rng_state(rng, dev))
     return desc, rows
+
+
+def _packed(desc, rows):
+    """The structs of a call in one buffer: (buffer, address of gtp_attn, address of each gtp_rows)."""
+    n = len(rows) // 3
+    buf = ctypes.create_string_buffer(_ATTN.size + ctypes.sizeof(_Rows) * n)
+    _ATTN.pack_into(buf, 0, *desc)
+    struct.pack_into("<" + _ROWS * n, buf, _ATTN.size, *rows)
+    at = ctypes.addressof(buf)
+    return buf, at, [at + _ATTN.size + ctypes.sizeof(_Rows) * i for i in range(n)]
 
 
 def gtp_attention(q, k, v, scale=None, q_off=None, k_off=None, max_q=None, max_k=None, key_mask=None, p: float = 0.0,
@@ -660,16 +690,18 @@ def gtp_attention(q, k, v, scale=None, q_off=None, k_off=None, max_q=None, max_k
     what the backward reads.  Tensors may be slices of a packed one (contiguous last dimension)."""
     import torch
     desc, rows = _attn(q, k, v, scale, q_off, k_off, max_q, max_k, key_mask, p, rng)
-    with _on_stream(stream):
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if o is None else o
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
-        ro = _attn_rows(o, "o", q.shape, q.dtype, q.device)
-        pl = _want(lse, "lse", q.shape[:2], _f32(), q.device)
+    dev, shape = q.device, q.shape
+    with _allocating(stream):
+        o = torch.empty(shape, dtype=q.dtype, device=dev) if o is None else o
+        lse = torch.empty(shape[:2], dtype=torch.float32, device=dev) if lse is None else lse
+        ro = _attn_rows(o, "o", shape, q.dtype, dev)
+        pl = _want(lse, "lse", shape[:2], (torch.float32,), dev)
         _on_gpu(q, "q")
-        nbytes = lib().gtp_attention_work(ctypes.byref(desc), 0)
-        work = _work(nbytes, q.device)
-    _check(lib().gtp_attention(ctypes.byref(desc), *map(ctypes.byref, rows), ctypes.byref(ro), pl, _ptr(work), nbytes,
-                               _stream(stream)))
+        buf, a, r = _packed(desc, (*rows, *ro))
+        lib_ = lib()
+        nbytes = lib_.gtp_attention_work(a, 0)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes > 0 else None
+    _check(lib_.gtp_attention(a, *r, pl, _ptr(work), nbytes, _stream(stream)), lib_)
     return o, lse
 
 
@@ -684,24 +716,30 @@ def gtp_attention_backward(q, k, v, o, do, lse, scale=None, q_off=None, k_off=No
     need = set(need)
     if need - {"dq", "dk", "dv"}:
         raise ValueError(f"unknown gradients {sorted(need - {'dq', 'dk', 'dv'})}")
-    ro = _attn_rows(o, "o", q.shape, q.dtype, q.device)
-    rdo = _attn_rows(do, "do", q.shape, q.dtype, q.device)
-    pl = _want(lse, "lse", q.shape[:2], _f32(), q.device)
-    with _on_stream(stream):
+    dev, dt, qs, ks = q.device, q.dtype, q.shape, k.shape
+    ro = _attn_rows(o, "o", qs, dt, dev)
+    rdo = _attn_rows(do, "do", qs, dt, dev)
+    pl = _want(lse, "lse", qs[:2], (torch.float32,), dev)
+    keys = "dk" in need or "dv" in need
+    none = (0, 0, 0)
+    with _allocating(stream):
         out = {}
-        for name, like, given in (("dq", q, dq), ("dk", k, dk), ("dv", v, dv)):
-            if name in need or (name != "dq" and need & {"dk", "dv"}):
-                out[name] = torch.empty(like.shape, dtype=q.dtype, device=q.device) if given is None else given
-        ptr = {n: _attn_rows(out[n], n, t.shape, q.dtype, q.device) if n in out else None
-               for n, t in (("dq", q), ("dk", k), ("dv", v))}
+        if "dq" in need:
+            out["dq"] = torch.empty(qs, dtype=dt, device=dev) if dq is None else dq
+        if keys:
+            out["dk"] = torch.empty(ks, dtype=dt, device=dev) if dk is None else dk
+            out["dv"] = torch.empty(ks, dtype=dt, device=dev) if dv is None else dv
+        rdq = _attn_rows(out["dq"], "dq", qs, dt, dev) if "dq" in need else none
+        rdk = _attn_rows(out["dk"], "dk", ks, dt, dev) if keys else none
+        rdv = _attn_rows(out["dv"], "dv", ks, dt, dev) if keys else none
         _on_gpu(q, "q")
-        nbytes = lib().gtp_attention_work(ctypes.byref(desc), 1)
-        work = _work(nbytes, q.device)
-    _check(lib().gtp_attention_backward(ctypes.byref(desc), *map(ctypes.byref, rows), ctypes.byref(ro),
-                                        ctypes.byref(rdo), pl,
-                                        *(_null() if ptr[n] is None else ctypes.byref(ptr[n]) for n in ("dq", "dk", "dv")),
-                                        _ptr(work), nbytes, _stream(stream)))
-    return {n: out[n] for n in out if n in need}
+        buf, a, r = _packed(desc, (*rows, *ro, *rdo, *rdq, *rdk, *rdv))
+        lib_ = lib()
+        nbytes = lib_.gtp_attention_work(a, 1)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes > 0 else None
+    _check(lib_.gtp_attention_backward(a, *r[:5], pl, r[5] if "dq" in need else None, *(r[6:] if keys else (None, None)),
+                                       _ptr(work), nbytes, _stream(stream)), lib_)
+    return {n: t for n, t in out.items() if n in need}
 
 
 def gtp_stream_probe(mode: int, src, dst, stream=None):
