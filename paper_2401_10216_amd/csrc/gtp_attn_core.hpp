@@ -120,6 +120,25 @@ __device__ __forceinline__ void mma(const Operand<T>& a, const Operand<T>& b, f3
   acc = mfma16(a.p[0], b.p[0], acc);
 }
 
+// Two products at once, instruction by instruction: one's partial product runs while the
+// other's waits for the sum before it.
+template <typename T>
+__device__ __forceinline__ void mma2(const Operand<T>& a, const Operand<T>& b, f32x16& acc, const Operand<T>& c,
+                                     const Operand<T>& d, f32x16& acc2) {
+  auto both = [&](int i, int j) {
+    acc = mfma16(a.p[i], b.p[j], acc);
+    acc2 = mfma16(c.p[i], d.p[j], acc2);
+  };
+  if constexpr (sizeof(T) == 4) {
+    both(0, 2);
+    both(2, 0);
+    both(1, 1);
+    both(0, 1);
+    both(1, 0);
+  }
+  both(0, 0);
+}
+
 // A tile of rows in LDS: a plane for each part, rows of DP bf16 values, 16 bytes of
 // padding behind each (the lanes of an operand's read take the same columns of 32 rows:
 // an odd stride in units of 16 bytes spreads them over the banks).
@@ -166,29 +185,43 @@ struct Columns {
   }
 };
 
-// acc[d, column] += sum over rows r0 .. r0 + 31 of a tile of tile[row][32 dt + d] v[row, column].
+// The M-side operand of columns 32 dt .. 32 dt + 31 of rows r0 + 16 s .. r0 + 16 s + 15 of
+// a tile, turned over, in the order in which a result holds its rows.
 template <typename T, int DP, int ROWS>
-__device__ __forceinline__ void mma_transposed(const char* tile, int r0, int dt, const Columns<T>& v, int lane,
-                                               f32x16& acc) {
+__device__ __forceinline__ Operand<T> turned_operand(const char* tile, int r0, int dt, int s, int lane) {
   constexpr int S = row_bytes<DP>();
   // 16 lanes read a block of 4 rows x 16 columns, 8 bytes each, and each receives
   // the 4 rows of its own column
-  const char* base = tile + (r0 + 4 * (lane >> 5) + ((lane & 15) >> 2)) * S +
+  const char* base = tile + (r0 + 16 * s + 4 * (lane >> 5) + ((lane & 15) >> 2)) * S +
                      (32 * dt + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
   typedef __attribute__((address_space(3))) s16x4* lds4;
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  Operand<T> a;
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    Operand<T> a;
-#pragma unroll
-    for (int p = 0; p < parts<T>(); ++p) {
-      const char* at = base + (p * ROWS + 16 * s) * S;
-      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at)));
-      const u32x2 up = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * S)));
-      a.p[p] = u32x4{lo[0], lo[1], up[0], up[1]};
-    }
-    mma<T>(a, v.s[s], acc);
+  for (int p = 0; p < parts<T>(); ++p) {
+    const char* at = base + p * ROWS * S;
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at)));
+    const u32x2 up = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * S)));
+    a.p[p] = u32x4{lo[0], lo[1], up[0], up[1]};
   }
+  return a;
+}
+
+// acc[i][d, column] += sum over rows r0 .. r0 + 31 of a tile of tile[row][32 (dt + i) + d] v[row, column].
+template <typename T, int DP, int ROWS, int N>
+__device__ __forceinline__ void mma_turned(const char* tile, int r0, int dt, const Columns<T>& v, int lane,
+                                           f32x16 (&acc)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 2)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const Operand<T> a = turned_operand<T, DP, ROWS>(tile, r0, dt + i, s, lane);
+      if (i + 1 < N)
+        mma2<T>(a, v.s[s], acc[i], turned_operand<T, DP, ROWS>(tile, r0, dt + (i + 1 < N ? i + 1 : i), s, lane), v.s[s],
+                acc[i + 1 < N ? i + 1 : i]);
+      else
+        mma<T>(a, v.s[s], acc[i]);
+    }
 }
 
 // 16 bytes of a row of d elements, column `col` in units of 16 bytes: get() issues
@@ -291,11 +324,17 @@ struct RowOperands {
         for (int p = 0; p < parts<T>(); ++p) o[c].p[p] ^= 0x80008000u;
     }
   }
+  // AGAIN: split at each use; else the compiler makes the parts once and keeps them in
+  // scratch memory (dk, dv of heads of 217: 1565 us so and 1200 split again; dq of them 795 and 868).
+  template <bool AGAIN = false>
   __device__ __forceinline__ Operand<T> operator()(int c) const {
-    if constexpr (RAW)
-      return split(raw[c][0], raw[c][1]);
-    else
+    if constexpr (RAW) {
+      u32x4 a = raw[c][0], b = raw[c][1];
+      if constexpr (AGAIN) asm volatile("" : "+v"(a), "+v"(b));
+      return split(a, b);
+    } else {
       return o[c];
+    }
   }
 };
 

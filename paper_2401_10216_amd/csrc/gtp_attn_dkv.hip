@@ -92,9 +92,11 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
     for (int t = 0; t < RT; ++t) {
       f32x16 s = zero16(), dp = zero16();
 #pragma unroll
-      for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BR>(tq, 32 * t + l31, c, hi), kf(c), s);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BR>(tg, 32 * t + l31, c, hi), vf(c), dp);
+      for (int c = 0; c < NC; ++c) {
+        mma2<T>(tile_operand<T, DP, BR>(tq, 32 * t + l31, c, hi), kf.template operator()<true>(c), s,
+                tile_operand<T, DP, BR>(tg, 32 * t + l31, c, hi), vf.template operator()<true>(c), dp);
+        if constexpr (long_rows<T, DP>()) __builtin_amdgcn_sched_barrier(0);  // a step's parts with the step: made ahead they spill
+      }
       uint32_t keep = 0xffffu;
       if constexpr (DROP) keep = drop.rows_of_key(r0 + 32 * t, int64_t(tile) * BK + wave * 32, lane);
       f32x16 p;
@@ -124,12 +126,10 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
       }
       {
         const Columns<T> pc(p);
-#pragma unroll
-        for (int i = 0; i < NDT; ++i) mma_transposed<T, DP, BR>(tg, 32 * t, part * NDT + i, pc, lane, av[i]);
+        mma_turned<T, DP, BR>(tg, 32 * t, part * NDT, pc, lane, av);
       }
       const Columns<T> ds(s);
-#pragma unroll
-      for (int i = 0; i < NDT; ++i) mma_transposed<T, DP, BR>(tq, 32 * t, part * NDT + i, ds, lane, ak[i]);
+      mma_turned<T, DP, BR>(tq, 32 * t, part * NDT, ds, lane, ak);
     }
   }
   if (!there) return;

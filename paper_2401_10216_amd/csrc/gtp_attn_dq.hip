@@ -88,9 +88,8 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
     if (AHEAD && j0 + BN < j_end) fetch(j0 + BN);  // in flight while this tile is worked on
     f32x16 s = zero16(), dp = zero16();
 #pragma unroll
-    for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BN>(tk, l31, c, hi), qf(c), s);
-#pragma unroll
-    for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BN>(tv, l31, c, hi), gf(c), dp);
+    for (int c = 0; c < NC; ++c)
+      mma2<T>(tile_operand<T, DP, BN>(tk, l31, c, hi), qf(c), s, tile_operand<T, DP, BN>(tv, l31, c, hi), gf(c), dp);
     uint32_t keep = 0xffffu;
     if constexpr (DROP) keep = drop.keys_of_row(R0, j0, lane);
 #pragma unroll
@@ -105,8 +104,7 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
       for (int r = 0; r < 16; ++r) s[r] = (ok >> tile_row(r, 0)) & 1u ? s[r] : 0.0f;
     }
     const Columns<T> ds(s);
-#pragma unroll
-    for (int i = 0; i < NDT; ++i) mma_transposed<T, DP, BN>(tk, 0, i, ds, lane, acc[i]);
+    mma_turned<T, DP, BN>(tk, 0, 0, ds, lane, acc);
   }
   if (!there) return;
   if (a.splits > 1) {

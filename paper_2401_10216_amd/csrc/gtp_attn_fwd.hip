@@ -77,10 +77,14 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const A
     uint32_t ok[KT];
     float top = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < KT; ++t) {
-      s[t] = zero16();
+    for (int t = 0; t < KT; ++t) s[t] = zero16();
 #pragma unroll
-      for (int c = 0; c < NC; ++c) mma<T>(tile_operand<T, DP, BN>(tk, 32 * t + l31, c, hi), qf(c), s[t]);
+    for (int c = 0; c < NC; ++c) {
+      const Operand<T> q = qf(c);
+      if constexpr (KT == 2)
+        mma2<T>(tile_operand<T, DP, BN>(tk, l31, c, hi), q, s[0], tile_operand<T, DP, BN>(tk, 32 + l31, c, hi), q, s[1]);
+      else
+        mma<T>(tile_operand<T, DP, BN>(tk, l31, c, hi), q, s[0]);
     }
     if (!whole) {
 #pragma unroll
@@ -121,8 +125,7 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const A
         if constexpr (DROP) s[t][r] = Drop::kept(s[t][r], keep, r);
       }
       const Columns<T> p(s[t]);
-#pragma unroll
-      for (int i = 0; i < NDT; ++i) mma_transposed<T, DP, BN>(tv, 32 * t, i, p, lane, acc[i]);
+      mma_turned<T, DP, BN>(tv, 32 * t, 0, p, lane, acc);
     }
   }
   l = half_sum(l);
