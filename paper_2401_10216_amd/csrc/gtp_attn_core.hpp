@@ -345,37 +345,33 @@ template <typename T, int DP, int ROWS, int NT>
 struct Stage {
   static constexpr int CPR = DP * int(sizeof(T)) / 16;
   static constexpr int ITER = (ROWS * CPR + NT - 1) / NT;
-  static_assert(ITER <= 32, "a bit for each load");
+  static_assert(ROWS <= 64, "a bit for each row");
   u32x4 reg[ITER];
-  uint32_t ok = 0;
   template <typename F>
   __device__ __forceinline__ void fetch(F row, int d, bool vec) {
-    ok = 0;
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
       const int id = int(threadIdx.x) + i * NT;
-      bool there = false;
-      const T* p = row(ROWS * CPR % NT != 0 && id >= ROWS * CPR ? 0 : id / CPR, &there);
+      const T* p = row(ROWS * CPR % NT != 0 && id >= ROWS * CPR ? 0 : id / CPR);
       reg[i] = Load16<T>::get(p, id % CPR, d, vec);
-      ok |= (there ? 1u : 0u) << i;
     }
   }
-  // whole: every row of the tile is there
-  __device__ __forceinline__ void commit(char* tile, int d, bool vec, bool whole) const {
+  // rows: a bit for each row of the tile, zeros where it is not there; whole: all are
+  __device__ __forceinline__ void commit(char* tile, int d, bool vec, bool whole, uint64_t rows) const {
     if (vec && whole && d == DP)
-      write<true>(tile, d, vec);
+      write<true>(tile, d, vec, rows);
     else
-      write<false>(tile, d, vec);
+      write<false>(tile, d, vec, rows);
   }
   template <bool PLAIN>
-  __device__ __forceinline__ void write(char* tile, int d, bool vec) const {
+  __device__ __forceinline__ void write(char* tile, int d, bool vec, uint64_t rows) const {
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
       const int id = int(threadIdx.x) + i * NT;
       if (ROWS * CPR % NT != 0 && id >= ROWS * CPR) break;
       char* const at = tile + (id / CPR) * row_bytes<DP>();
-      const u32x4 v = PLAIN ? reg[i] : Load16<T>::fix(reg[i], id % CPR, d, vec, (ok >> i) & 1u);
+      const u32x4 v = PLAIN ? reg[i] : Load16<T>::fix(reg[i], id % CPR, d, vec, (rows >> (id / CPR)) & 1u);
       if constexpr (sizeof(T) == 2) {
         *reinterpret_cast<u32x4*>(at + 16 * (id % CPR)) = v;
       } else {
@@ -400,6 +396,22 @@ __device__ __forceinline__ void segment(const int64_t* off, int64_t b, int64_t m
   start = s;
   n = e - s < most ? e - s : most;
 }
+
+// Which keys of a tile are there: a lane loads the mask's byte of key lane % ROWS, ahead
+// with the tile and whether or not there is a mask (a load under a condition is waited
+// for on the spot; one for each staged piece of a row was most of a short call's time).
+template <int ROWS>
+struct Present {
+  uint32_t byte = 0;
+  // j0 < n; base: any memory of ours to read where there is no mask
+  __device__ __forceinline__ void fetch(const uint8_t* mask, const void* base, int64_t j0, int64_t n, int lane) {
+    const int64_t j = j0 + (lane & (ROWS - 1));
+    byte = *(mask ? mask + (j < n ? j : j0) : static_cast<const uint8_t*>(base));
+  }
+  __device__ __forceinline__ uint64_t rows(const uint8_t* mask, int64_t j0, int64_t n, int lane) const {
+    return __ballot(j0 + (lane & (ROWS - 1)) < n && (!mask || byte != 0));
+  }
+};
 
 // Row R = i G + g of a key head's rows: i, and g in *g.  (64-bit divisions in the tile
 // loop took longer than its products; R < 2^31 by the launch's limits.)

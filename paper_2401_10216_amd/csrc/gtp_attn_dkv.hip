@@ -52,26 +52,20 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
   const int64_t r_end = (w.split + 1) * per * BR < rows ? (w.split + 1) * per * BR : rows;
   const Group group(a.G);
   Stage<T, DP, BR, NT> sq, sg;
-  float ref = INFINITY, delta = 0.0f;
+  float lse = 0.0f, delta = 0.0f;
   auto fetch = [&](int64_t r0) {
-    auto row = [&](const AttnRows& t, int r, bool* ok) {
-      *ok = r0 + r < rows;
-      const int64_t R = *ok ? r0 + r : r0;
+    auto row = [&](const AttnRows& t, int r) {
       int g;
-      const int64_t i = group.row(R, &g);
+      const int64_t i = group.row(r0 + r < rows ? r0 + r : r0, &g);
       return static_cast<const T*>(t.p) + (qs + i) * t.row + (w.hk * a.G + g) * t.head;
     };
-    sq.fetch([&](int r, bool* ok) { return row(a.q, r, ok); }, a.d, a.vec);
-    sg.fetch([&](int r, bool* ok) { return row(a.dout, r, ok); }, a.d, a.vec);
-    ref = INFINITY;
-    delta = 0.0f;
-    if (threadIdx.x < BR && r0 + threadIdx.x < rows) {
-      int g;
-      const int64_t i = group.row(r0 + threadIdx.x, &g), at = (qs + i) * a.H + w.hk * a.G + g;
-      const float lse = a.lse[at];
-      ref = lse == -INFINITY ? INFINITY : lse * kLog2e;
-      delta = a.delta[at];
-    }
+    sq.fetch([&](int r) { return row(a.q, r); }, a.d, a.vec);
+    sg.fetch([&](int r) { return row(a.dout, r); }, a.d, a.vec);
+    int g;  // by every thread, wanted or not: under a condition these loads, and the tile's, were waited for here
+    const int64_t rt = r0 + (threadIdx.x & (BR - 1)), i = group.row(rt < rows ? rt : r0, &g);
+    const int64_t at = (qs + i) * a.H + w.hk * a.G + g;
+    lse = a.lse[at];
+    delta = a.delta[at];
   };
   int64_t r0 = w.split * per * BR;
   constexpr bool AHEAD = !long_rows<T, DP>() && !(sizeof(T) == 2 && DP == 128);  // there the registers hold no more
@@ -80,11 +74,13 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
     if (!AHEAD) fetch(r0);
     __syncthreads();
     const bool whole = r0 + BR <= rows;
-    sq.commit(tq, a.d, a.vec, whole);
-    sg.commit(tg, a.d, a.vec, whole);
+    const uint64_t there_r = whole ? ~uint64_t(0) : (uint64_t(1) << (rows - r0)) - 1;  // fewer than 64 left
+    sq.commit(tq, a.d, a.vec, whole, there_r);
+    sg.commit(tg, a.d, a.vec, whole, there_r);
     if (threadIdx.x < BR) {
-      t_ref[threadIdx.x] = ref;
-      t_delta[threadIdx.x] = delta;
+      const bool in = r0 + threadIdx.x < rows;
+      t_ref[threadIdx.x] = !in || lse == -INFINITY ? INFINITY : lse * kLog2e;
+      t_delta[threadIdx.x] = in ? delta : 0.0f;
     }
     __syncthreads();
     if (AHEAD && r0 + BR < r_end) fetch(r0 + BR);  // in flight while this tile is worked on

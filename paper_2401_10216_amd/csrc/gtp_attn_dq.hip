@@ -66,14 +66,11 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
   const int64_t ntile = (nk + BN - 1) / BN, per = (ntile + a.splits - 1) / a.splits;
   const int64_t j_end = (w.split + 1) * per * BN < nk ? (w.split + 1) * per * BN : nk;
   Stage<T, DP, BN, NT> sk, sv;
-  auto present = [&](int64_t j) { return j < nk && (!mask || mask[j]); };
+  Present<BN> here;
   auto fetch = [&](int64_t j0) {
-    auto row = [&](const T* base, int64_t stride, int r, bool* ok) {
-      *ok = present(j0 + r);
-      return base + (j0 + r < nk ? j0 + r : j0) * stride;
-    };
-    sk.fetch([&](int r, bool* ok) { return row(kb, a.k.row, r, ok); }, a.d, a.vec);
-    sv.fetch([&](int r, bool* ok) { return row(vb, a.v.row, r, ok); }, a.d, a.vec);
+    here.fetch(mask, kb, j0, nk, lane);
+    sk.fetch([&](int r) { return kb + (j0 + r < nk ? j0 + r : j0) * a.k.row; }, a.d, a.vec);
+    sv.fetch([&](int r) { return vb + (j0 + r < nk ? j0 + r : j0) * a.v.row; }, a.d, a.vec);
   };
   int64_t j0 = w.split * per * BN;
   constexpr bool AHEAD = !long_rows<T, DP>();
@@ -82,8 +79,9 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
     if (!AHEAD) fetch(j0);
     __syncthreads();
     const bool whole = !mask && j0 + BN <= nk;
-    sk.commit(tk, a.d, a.vec, whole);
-    sv.commit(tv, a.d, a.vec, whole);
+    const uint64_t keys = here.rows(mask, j0, nk, lane);  // zeros stand for absent keys' rows
+    sk.commit(tk, a.d, a.vec, whole, keys);
+    sv.commit(tv, a.d, a.vec, whole, keys);
     __syncthreads();
     if (AHEAD && j0 + BN < j_end) fetch(j0 + BN);  // in flight while this tile is worked on
     f32x16 s = zero16(), dp = zero16();
@@ -99,7 +97,7 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
       s[r] = p * (g - delta);
     }
     if (!whole) {
-      const uint32_t ok = uint32_t(__ballot(present(j0 + l31))) >> (4 * hi);
+      const uint32_t ok = uint32_t(keys) >> (4 * hi);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = (ok >> tile_row(r, 0)) & 1u ? s[r] : 0.0f;
     }
