@@ -41,7 +41,7 @@ inline int rows_a_tile(int64_t most) { return most <= 64 ? 64 : 128; }
 int attn_padded(int d);  // the head length that the kernels are instantiated at, >= d
 // Parts that the keys of each row (the rows of each key) are dealt to: 1 where the
 // workgroups fill the chip without.
-int attn_row_splits(const AttnArgs& a);
+int attn_row_splits(const AttnArgs& a, bool backward);  // its parts: of the forward, of dq
 int attn_key_splits(const AttnArgs& a);
 hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_delta(const AttnArgs& a, hipStream_t s);

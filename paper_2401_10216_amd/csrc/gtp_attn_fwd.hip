@@ -11,6 +11,18 @@ namespace {
 
 constexpr float kSlack = 8.0f;  // probabilities stay below 2^8: far from overflow in fp32 and bf16, and as exact
 
+constexpr int kParts = 128;     // at most, of a split call
+
+template <typename T>
+__device__ __forceinline__ void store_one(T* p, float v) {
+  if constexpr (sizeof(T) == 4) {
+    *p = v;
+  } else {
+    const __bf16 one = static_cast<__bf16>(v);
+    *p = __builtin_bit_cast(uint16_t, one);
+  }
+}
+
 // Workgroup: 32 NW rows of one key head (a wave 32), keys in tiles of 32 KT.
 template <typename T, int DP, int KT, bool DROP, int NW>
 __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const AttnArgs a, int64_t n_wg, int tiles) {
@@ -140,50 +152,76 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const A
   if (hi == 0) a.lse[qi * a.H + h] = lse;
 }
 
-// Joins the parts of a split forward: o = sum_s e^(lse_s - lse) o_s.  A wave takes a
-// row, its lanes first the parts, then the elements.
-template <typename T>
+// Joins the parts of a split forward: o = sum_s e^(lse_s - lse) o_s.  WAVES waves take a
+// row: their lanes first the parts, two each (at most kParts), then the elements, each wave its parts of
+// them in order; the waves' sums are added in order.  What it costs is the wait for loads
+// one after the other, so many parts are dealt to more waves.
+template <typename T, int WAVES>
 __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a) {
-  const int64_t per = (a.max_q * a.H + 3) / 4, b = blockIdx.x / per;
-  const int64_t i = (blockIdx.x % per) * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
+  static_assert(kParts <= 128, "two parts a lane");
+  constexpr int ROWS = 4 / WAVES;
+  __shared__ float sums[WAVES > 1 ? WAVES * 256 : 1];
+  lds_poison(sums, int(sizeof(sums) / 4));
+  const int64_t per = (a.max_q * a.H + ROWS - 1) / ROWS, b = blockIdx.x / per;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first = wave % WAVES;
+  const int64_t i = (blockIdx.x % per) * ROWS + wave / WAVES;
   int64_t qs, nq;
   segment(a.q_off, b, a.max_q, a.Tq, qs, nq);
-  if (i >= nq * a.H) return;
+  if (i >= nq * a.H) return;  // a whole workgroup, where waves share a row
   const int64_t t = qs + i / a.H, h = i % a.H, all = a.Tq * a.H, row = t * a.H + h;
   const float* const lses = a.part + a.splits * all * a.d;
-  const float own = lane < a.splits ? lses[lane * all + row] : -INFINITY;
-  float top = own;
+  float own[2], e[2], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int s = lane + 64 * k;
+    const float got = lses[int64_t(s < a.splits ? s : 0) * all + row];
+    own[k] = s < a.splits ? got : -INFINITY;
+    top = fmaxf(top, own[k]);
+  }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  const float e = own == -INFINITY ? 0.0f : expf(own - top);  // NaN where a part's row is
-  float sum = e;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    e[k] = own[k] == -INFINITY ? 0.0f : expf(own[k] - top);  // NaN where a part's row is
+    sum += e[k];
+  }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  const float weight = sum == 0.0f ? 0.0f : e / sum;
-  if (lane == 0) a.lse[row] = sum == 0.0f ? -INFINITY : top + logf(sum);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) e[k] = sum == 0.0f ? 0.0f : e[k] / sum;
+  if (lane == 0 && first == 0) a.lse[row] = sum == 0.0f ? -INFINITY : top + logf(sum);
   T* const out = static_cast<T*>(const_cast<void*>(a.out.p)) + t * a.out.row + h * a.out.head;
   for (int c0 = 0; c0 < a.d; c0 += 64) {
     const int c = c0 + lane;
     const float* const in = a.part + row * a.d + (c < a.d ? c : 0);
     float v = 0.0f;
-    for (int s0 = 0; s0 < a.splits; s0 += 8) {  // eight parts' loads at a time
+    for (int s0 = first; s0 < a.splits; s0 += 8 * WAVES) {  // eight parts' loads at a time
       float p[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) p[k] = in[int64_t(s0 + k < a.splits ? s0 + k : 0) * all * a.d];
+      for (int k = 0; k < 8; ++k) {
+        const int s = s0 + k * WAVES;
+        p[k] = in[int64_t(s < a.splits ? s : 0) * all * a.d];
+      }
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float ws = __shfl(weight, (s0 + k) & 63);  // 0 past the last part
-        v = s0 + k >= a.splits || ws == 0.0f ? v : fmaf(ws, p[k], v);
+        const int s = s0 + k * WAVES;
+        const float low = __shfl(e[0], s & 63), high = __shfl(e[1], s & 63), ws = s < 64 ? low : high;
+        v = s >= a.splits || ws == 0.0f ? v : fmaf(ws, p[k], v);
       }
     }
-    if (c < a.d) {
-      if constexpr (sizeof(T) == 4) {
-        out[c] = v;
-      } else {
-        const __bf16 one = static_cast<__bf16>(v);
-        out[c] = __builtin_bit_cast(uint16_t, one);
-      }
+    if constexpr (WAVES > 1) {
+      sums[wave * 256 + c] = v;  // c < 256: heads are at most 256 long
+      continue;
+    }
+    if (c < a.d) store_one<T>(out + c, v);
+  }
+  if constexpr (WAVES > 1) {
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.d; c += 256) {
+      float v = sums[c];
+#pragma unroll
+      for (int k = 1; k < WAVES; ++k) v += sums[k * 256 + c];
+      store_one<T>(out + c, v);
     }
   }
 }
@@ -203,34 +241,34 @@ __global__ __launch_bounds__(256) void k_attn_sum(const float* __restrict__ part
     float v = 0.0f;
 #pragma unroll 8
     for (int s = 0; s < splits; ++s) v += part[(int64_t(s) * all + row) * d + c];
-    if constexpr (sizeof(T) == 4) {
-      o[c] = v;
-    } else {
-      const __bf16 one = static_cast<__bf16>(v);
-      o[c] = __builtin_bit_cast(uint16_t, one);
-    }
+    store_one<T>(o + c, v);
   }
 }
 
-// Parts for n workgroups whose loops take `tiles` tiles, at `per_cu` of them a CU at a
-// time: as few as keep the CUs nine tenths busy to the end of the last round (n a
-// little above a round leaves most of them idle in the second), two tiles each at least.
-int parts_for(int64_t n, int64_t tiles, int per_cu) {
-  const int64_t slots = 256 * per_cu;
+// Parts for n workgroups whose loops take `length` rows in tiles of `step`, at `per_cu`
+// of them a CU at a time: as few as keep the CUs nine tenths busy, tiles of the longest
+// part counted, to the end of the last round (n a little above a round leaves most of
+// them idle in the second); a part has 128 rows at least and saves a twentieth at least.
+int parts_for(int64_t n, int64_t length, int step, int per_cu) {
+  const int64_t slots = 256 * per_cu, tiles = (length + step - 1) / step;
   if (n <= 0 || n >= 8 * slots) return 1;
   int64_t best = 1;
   double use = 0.0;
-  for (int64_t s = 1; s <= 64 && (s == 1 || s <= tiles / 2); ++s) {
-    const double rounds = double(n * s) / double(slots), u = rounds / std::ceil(rounds);
-    if (u > use + 0.02) use = u, best = s;
+  for (int64_t s = 1; s <= kParts && (s == 1 || s <= length / 128); ++s) {
+    const int64_t rounds = (n * s + slots - 1) / slots, longest = (tiles + s - 1) / s;
+    const double u = double(n) * double(tiles) / (double(slots) * double(rounds) * double(longest));
+    if (u > 1.05 * use) use = u, best = s;
     if (use >= 0.9) break;
   }
   return int(best);
 }
 
+// Tiles of 32 keys that the forward takes at a time.
+constexpr int key_tiles(int DP, bool bf16) { return !bf16 && DP > 64 ? 1 : 2; }
+
 template <typename T, int DP, bool DROP>
 void launch_tiles(const AttnArgs& a, hipStream_t s) {
-  constexpr int KT = sizeof(T) == 4 && DP > 64 ? 1 : 2;
+  constexpr int KT = key_tiles(DP, sizeof(T) == 2);
   const int64_t BM = rows_a_tile(a.max_q * a.G), tiles = (a.max_q * a.G + BM - 1) / BM, n = tiles * a.splits * a.Hk * a.B;
   if (BM == 64)
     k_attn_fwd<T, DP, KT, DROP, 2><<<uint32_t(n), 128, 0, s>>>(a, n, int(tiles));
@@ -245,8 +283,10 @@ hipError_t launch(const AttnArgs& a, hipStream_t s) {
   else
     launch_tiles<T, DP, false>(a, s);
   if (a.splits > 1) {
-    const int64_t rows = (a.max_q * a.H + 3) / 4 * a.B;
-    k_attn_join<T><<<uint32_t(rows), 256, 0, s>>>(a);
+    if (a.splits > 16)
+      k_attn_join<T, 4><<<uint32_t(a.max_q * a.H * a.B), 256, 0, s>>>(a);
+    else
+      k_attn_join<T, 1><<<uint32_t((a.max_q * a.H + 3) / 4 * a.B), 256, 0, s>>>(a);
   }
   return hipGetLastError();
 }
@@ -255,22 +295,17 @@ hipError_t launch(const AttnArgs& a, hipStream_t s) {
 
 int attn_padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256; }
 
-// Workgroups that a CU holds, by the registers that the kernels are cut for.
-namespace {
-int wg_a_cu(const AttnArgs& a, bool keys) {
-  const int bytes = attn_padded(a.d) * (a.bf16 ? 2 : 4);
-  return bytes <= (keys && !a.bf16 ? 128 : 256) ? 2 : 1;
-}
-}  // namespace
-
-int attn_row_splits(const AttnArgs& a) {
-  const int BM = rows_a_tile(a.max_q * a.G);
-  return parts_for((a.max_q * a.G + BM - 1) / BM * a.Hk * a.B, (a.max_k + 63) / 64, wg_a_cu(a, false));
+// Workgroups that a CU holds: by the waves a SIMD that the kernels' registers are cut for.
+int attn_row_splits(const AttnArgs& a, bool backward) {
+  const int BM = rows_a_tile(a.max_q * a.G), DP = attn_padded(a.d);
+  const int waves = DP * (a.bf16 ? 2 : 4) <= 256 || (!backward && DP <= 128) ? 2 : 1;
+  return parts_for((a.max_q * a.G + BM - 1) / BM * a.Hk * a.B, a.max_k, backward ? 32 : 32 * key_tiles(DP, a.bf16),
+                   waves * 128 / BM);
 }
 int attn_key_splits(const AttnArgs& a) {
-  const int BK = rows_a_tile(a.max_k);
-  return parts_for((a.max_k + BK - 1) / BK * (attn_padded(a.d) > 128 ? 2 : 1) * a.Hk * a.B, (a.max_q * a.G + 63) / 64,
-                   wg_a_cu(a, true));
+  const int BK = rows_a_tile(a.max_k), DP = attn_padded(a.d), bytes = DP * (a.bf16 ? 2 : 4);
+  return parts_for((a.max_k + BK - 1) / BK * (DP > 128 ? 2 : 1) * a.Hk * a.B, a.max_q * a.G, bytes <= 128 ? 64 : 32,
+                   (bytes <= (a.bf16 ? 256 : 128) ? 2 : 1) * 128 / BK);
 }
 
 hipError_t launch_attn_sum(const AttnArgs& a, const float* part, int splits, bool keys, const AttnRows& out,

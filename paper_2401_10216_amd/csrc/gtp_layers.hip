@@ -264,7 +264,7 @@ gtp::AttnRows rows_of(const gtp_rows* r) { return r ? gtp::AttnRows{r->data, r->
 // deltas, then the parts of dq or of dk and dv, one after the other in the same place.
 int64_t delta_bytes(const gtp::AttnArgs& g) { return (g.Tq * g.H * 4 + 15) / 16 * 16; }
 int64_t attn_work(const gtp::AttnArgs& g, int backward) {
-  const int64_t s = gtp::attn_row_splits(g), rows = s > 1 ? s * g.Tq * g.H * (g.d + (backward ? 0 : 1)) * 4 : 0;
+  const int64_t s = gtp::attn_row_splits(g, backward), rows = s > 1 ? s * g.Tq * g.H * (g.d + (backward ? 0 : 1)) * 4 : 0;
   if (!backward) return rows;
   const int64_t t = gtp::attn_key_splits(g), keys = t > 1 ? 2 * t * g.Tk * g.Hk * g.d * 4 : 0;
   return delta_bytes(g) + (rows > keys ? rows : keys);
@@ -340,7 +340,7 @@ gtp_status gtp_attention(const gtp_attn* a, const gtp_rows* q, const gtp_rows* k
   g.out = rows_of(o);
   g.lse = lse;
   g.part = static_cast<float*>(work);
-  g.splits = gtp::attn_row_splits(g);
+  g.splits = gtp::attn_row_splits(g, false);
   return launched(gtp::launch_attn_fwd(g, static_cast<hipStream_t>(stream)), "gtp_attention");
 }
 
@@ -374,7 +374,7 @@ gtp_status gtp_attention_backward(const gtp_attn* a, const gtp_rows* q, const gt
   hipError_t e = a->Tq > 0 ? gtp::launch_attn_delta(g, st) : hipSuccess;
   g.part = reinterpret_cast<float*>(static_cast<char*>(work) + delta_bytes(g));
   if (e == hipSuccess && dq && a->max_q > 0) {
-    g.splits = gtp::attn_row_splits(g);
+    g.splits = gtp::attn_row_splits(g, true);
     e = gtp::launch_attn_dq(g, st);
     if (e == hipSuccess && g.splits > 1) e = gtp::launch_attn_sum(g, g.part, g.splits, false, g.out, st);
   }
