@@ -2,14 +2,26 @@
 // from the scores and the rows' lse,
 //   P = exp(scale q k^T - lse),  dP = (dout v^T) m,  dS = P (dP - delta),
 //   dq = scale dS k,  delta = rows' sums of dout o,
-// m the factors 0 or 1 / (1 - p) of dropped probabilities.
+// m the factors 0 or 1 / (1 - p) of dropped probabilities (made again from the
+// generator, not stored).  dS is rounded to the operands' type for the last product
+// (fp32: in three parts).
+//
+// The rows lie as in the forward: a wave's 32 rows are the columns of its products,
+// their q and dout in registers, keys and values staged for all waves.  dq and dk, dv
+// each make S and dP for themselves: one kernel for all three would add to one of them
+// with atomics, whose order changes the result.  The matrix unit bounds the long cases
+// (6 d flops a row and key), with waits of the one wave a SIMD that fp32 heads longer
+// than 64 leave room for; where probabilities are dropped, the draws add vector work of
+// more than half of that (two segments of 5000-6500 rows, 16 heads of 64 over 4, bf16: 1028 us
+// with, 634 without).  4001 rows, 8 heads of 100, fp32: 624-664 us, 116-123 TFLOP/s.
 #include "gtp_attn_core.hpp"
 
 namespace gtp {
 namespace {
 
-
-// delta[t, h] = sum_i dout[t, h, i] o[t, h, i]: 16 lanes a row.
+// delta[t, h] = sum_i dout[t, h, i] o[t, h, i]: 16 lanes a row.  In a
+// pass of its own, once for both gradients: dout and o read once, HBM's time for the long
+// cases and a launch's (4 us) for the short.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_delta(const AttnArgs a) {
   const int64_t n = a.Tq * a.H, id = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4);

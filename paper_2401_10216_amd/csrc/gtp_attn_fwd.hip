@@ -2,6 +2,24 @@
 // row's segment, in one pass over the keys with the running maximum and sum of
 // each row, and lse = log of the row's sum (the backward pass makes the
 // probabilities again from it).
+//
+//   m' = max(m, scores of the tile),  l' = l 2^(m - m') + sum 2^(s - m'),
+//   o' = o 2^(m - m') + 2^(s - m') v,  o = o' / l'  (scores in units of log 2).
+// Probabilities are rounded to the operands' type (bf16: up to 2^-8 of each, as the inputs
+// themselves are; fp32: in three parts, below an fp32 rounding), their sum l is of the
+// unrounded ones in fp32.
+//
+// Long segments: the matrix unit bounds it (4 d flops a row and key), beside it the
+// exponentials and the operands' way through LDS.  A workgroup's four waves share the
+// staged keys and values, each for 32 rows, so a staged tile is used 128 times; two
+// waves a SIMD, one with vector instructions while the other's products run.  8192
+// rows, 8 heads of 128, bf16: 330-370 us, 740-830 TFLOP/s (library products of that
+// type here: 1200); 4096 rows, 8 heads of 128, fp32: 461-471 us, 146-149 TFLOP/s (154).
+// Few rows: the keys' way from HBM bounds it, so they are dealt to parts, in workgroups of
+// 64 rows, four a CU; one row of 8 heads of 128 against 60000 keys, bf16: 57-62 us, 4.0-4.3
+// TB/s.
+// Molecules of 5 to 49 atoms: one short pass, waits one after the other (offsets, rows,
+// keys, products): 64 of them, 8 heads of 72, fp32: 21.6 us.
 #include <cmath>
 
 #include "gtp_attn_core.hpp"
@@ -23,7 +41,8 @@ __device__ __forceinline__ void store_one(T* p, float v) {
   }
 }
 
-// Workgroup: 32 NW rows of one key head (a wave 32), keys in tiles of 32 KT.
+// Workgroup: 32 NW rows of one key head (a wave 32), keys in tiles of 32 KT.  Heads longer
+// than 128 leave the registers room for one wave a SIMD only.
 template <typename T, int DP, int KT, bool DROP, int NW>
 __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const AttnArgs a, int64_t n_wg, int tiles) {
   constexpr int NT = 64 * NW, BM = 32 * NW, BN = 32 * KT, NC = DP / 16, NDT = DP / 32;
@@ -246,19 +265,22 @@ __global__ __launch_bounds__(256) void k_attn_sum(const float* __restrict__ part
 }
 
 // Parts for n workgroups whose loops take `length` rows in tiles of `step`, at `per_cu`
-// of them a CU at a time: as few as keep the CUs nine tenths busy, tiles of the longest
-// part counted, to the end of the last round (n a little above a round leaves most of
-// them idle in the second); a part has 128 rows at least and saves a twentieth at least.
-int parts_for(int64_t n, int64_t length, int step, int per_cu) {
-  const int64_t slots = 256 * per_cu, tiles = (length + step - 1) / step;
+// of them a CU at a time: where the time is least, counted in tiles of the longest part,
+// times rounds of workgroups (a last one of fewer a CU is a little faster), with the
+// writing and reading of a part's results, which take what some 256 rows' products of 16
+// bits do or 64 of fp32.  A part has 128 rows at least and saves a twentieth at least.
+// Two segments of 5000-6500 rows, 16 heads of 64 over 4, bf16: whole 626 us, in the parts that
+// fill the last round 680; 4096 rows, 8 heads of 128, fp32: whole 632, in two parts 471.
+int parts_for(int64_t n, int64_t length, int step, int per_cu, bool bf16) {
+  const int64_t slots = 256 * per_cu, tiles = (length + step - 1) / step, join = (bf16 ? 256 : 64) / step;
   if (n <= 0 || n >= 8 * slots) return 1;
   int64_t best = 1;
-  double use = 0.0;
+  double least = INFINITY;
   for (int64_t s = 1; s <= kParts && (s == 1 || s <= length / 128); ++s) {
-    const int64_t rounds = (n * s + slots - 1) / slots, longest = (tiles + s - 1) / s;
-    const double u = double(n) * double(tiles) / (double(slots) * double(rounds) * double(longest));
-    if (u > 1.05 * use) use = u, best = s;
-    if (use >= 0.9) break;
+    const int64_t left = (n * s) % slots, longest = (tiles + s - 1) / s + (s > 1 ? join : 0);
+    const double last = left ? 0.5 * (1.0 + double((left + 255) / 256) / per_cu) : 0.0;
+    const double time = (double((n * s) / slots) + last) * double(longest);
+    if (time < 0.95 * least) least = time, best = s;
   }
   return int(best);
 }
@@ -283,6 +305,9 @@ hipError_t launch(const AttnArgs& a, hipStream_t s) {
   else
     launch_tiles<T, DP, false>(a, s);
   if (a.splits > 1) {
+    // four waves a row for many parts, whose loads one wave waits for eight at a time (32 rows
+    // of 64: 64 parts by one wave 6.1 us, 125 by four 4.6); few parts of many rows want
+    // fewer workgroups
     if (a.splits > 16)
       k_attn_join<T, 4><<<uint32_t(a.max_q * a.H * a.B), 256, 0, s>>>(a);
     else
@@ -300,12 +325,12 @@ int attn_row_splits(const AttnArgs& a, bool backward) {
   const int BM = rows_a_tile(a.max_q * a.G), DP = attn_padded(a.d);
   const int waves = DP * (a.bf16 ? 2 : 4) <= 256 || (!backward && DP <= 128) ? 2 : 1;
   return parts_for((a.max_q * a.G + BM - 1) / BM * a.Hk * a.B, a.max_k, backward ? 32 : 32 * key_tiles(DP, a.bf16),
-                   waves * 128 / BM);
+                   waves * 128 / BM, a.bf16);
 }
 int attn_key_splits(const AttnArgs& a) {
   const int BK = rows_a_tile(a.max_k), DP = attn_padded(a.d), bytes = DP * (a.bf16 ? 2 : 4);
   return parts_for((a.max_k + BK - 1) / BK * (DP > 128 ? 2 : 1) * a.Hk * a.B, a.max_q * a.G, bytes <= 128 ? 64 : 32,
-                   (bytes <= (a.bf16 ? 256 : 128) ? 2 : 1) * 128 / BK);
+                   (bytes <= (a.bf16 ? 256 : 128) ? 2 : 1) * 128 / BK, a.bf16);
 }
 
 hipError_t launch_attn_sum(const AttnArgs& a, const float* part, int splits, bool keys, const AttnRows& out,

@@ -15,7 +15,7 @@
 // time, 1 to 16 waves by its length; the sums of a degree go through LDS.  Measured:
 // 16384 x 128 channels of degree 6, fp32, 156-164 us forward (5.0-5.3 TB/s; the chip's
 // best copy 5.5) and 245-260 backward; 65536 rows of 256, 20 and 31 us.  Degree 16 with
-// 64 channels (18496 elements a row, bf16) runs at 200 us forward (3.0 TB/s) and 440-460
+// 64 channels (18496 elements a row, bf16) runs at 200 us forward (3.0 TB/s) and 440-463
 // backward (2.0): its one workgroup a CU cannot load a row while it sums another.
 #include <algorithm>
 #include <type_traits>
