@@ -269,8 +269,8 @@ __global__ __launch_bounds__(256) void k_attn_sum(const float* __restrict__ part
 // times rounds of workgroups (a last one of fewer a CU is a little faster), with the
 // writing and reading of a part's results, which take what some 256 rows' products of 16
 // bits do or 64 of fp32.  A part has 128 rows at least and saves a twentieth at least.
-// Two segments of 5000-6500 rows, 16 heads of 64 over 4, bf16: whole 626 us, in the parts that
-// fill the last round 680; 4096 rows, 8 heads of 128, fp32: whole 632, in two parts 471.
+// Two segments of 5000-6500 rows, 16 heads of 64 over 4, bf16: whole 626 us, in parts that
+// fill all rounds 680 us; 4096 rows, 8 heads of 128, fp32: whole 632, in two parts 471.
 int parts_for(int64_t n, int64_t length, int step, int per_cu, bool bf16) {
   const int64_t slots = 256 * per_cu, tiles = (length + step - 1) / step, join = (bf16 ? 256 : 64) / step;
   if (n <= 0 || n >= 8 * slots) return 1;
