@@ -1128,9 +1128,9 @@ struct Backward {
   hipStream_t s;
   template <typename T, int V, int NI>
   hipError_t operator()() const {
-    if constexpr (NI == 0) {
-      hipError_t e = a.y ? run_norm_backward<T, V, 0>(a, y, s) : hipSuccess;
-      if (e == hipSuccess && (a.dw || a.db)) e = run_norm_dw<T, V>(a, y, s);
+    if constexpr (NI == 0) {  // dw and db before dx, which may be written over dy
+      hipError_t e = a.dw || a.db ? run_norm_dw<T, V>(a, y, s) : hipSuccess;
+      if (e == hipSuccess && a.y) e = run_norm_backward<T, V, 0>(a, y, s);
       return e;
     } else {
       return run_norm_backward<T, V, NI>(a, y, s);
@@ -1192,19 +1192,20 @@ hipError_t launch_norm_backward(const NormArgs& a, hipStream_t s) {
   const int64_t used = a.N ? (a.N + chunk - 1) / chunk : 0;
   const dim3 grid{uint32_t(a.N)}, gw{uint32_t(a.C), uint32_t(used)};
   const bool weights = a.dw || a.db;
+  // dw and db before dx, which may be written over dy
   if (a.bf16) {
     const auto *x = static_cast<const uint16_t*>(a.x), *dy = static_cast<const uint16_t*>(a.dy);
+    if (weights && a.N)
+      k_norm_dw_any<<<gw, kAnyThreads, 0, s>>>(x, dy, a.mean_in, a.rstd_in, a.N, a.C, a.L, chunk, a.partial);
     if (a.y && a.N)
       k_norm_dx_any<<<grid, kAnyThreads, 0, s>>>(x, dy, a.w, a.mean_in, a.rstd_in, a.C, a.L,
                                                  static_cast<uint16_t*>(a.y));
-    if (weights && a.N)
-      k_norm_dw_any<<<gw, kAnyThreads, 0, s>>>(x, dy, a.mean_in, a.rstd_in, a.N, a.C, a.L, chunk, a.partial);
   } else {
     const auto *x = static_cast<const float*>(a.x), *dy = static_cast<const float*>(a.dy);
-    if (a.y && a.N)
-      k_norm_dx_any<<<grid, kAnyThreads, 0, s>>>(x, dy, a.w, a.mean_in, a.rstd_in, a.C, a.L, static_cast<float*>(a.y));
     if (weights && a.N)
       k_norm_dw_any<<<gw, kAnyThreads, 0, s>>>(x, dy, a.mean_in, a.rstd_in, a.N, a.C, a.L, chunk, a.partial);
+    if (a.y && a.N)
+      k_norm_dx_any<<<grid, kAnyThreads, 0, s>>>(x, dy, a.w, a.mean_in, a.rstd_in, a.C, a.L, static_cast<float*>(a.y));
   }
   return weights ? sum_parts(a, used, s) : hipGetLastError();
 }

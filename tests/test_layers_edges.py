@@ -1,0 +1,59 @@
+"""The layers around the product on the GPU at the edges of what their entries
+accept: gradients in place, infinities and values near fp32's largest, sizes
+past one launch, many rows a workgroup."""
+import ctypes
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from test_layers import BF16, F32, Case, _say, gen, norm_case, norm_check, randn  # noqa: E402,F401
+from paper_2401_10216_amd import gtp  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def device():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    gtp.lib()
+
+
+def stream():
+    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def code(t):
+    return {F32: 0, BF16: 1}[t.dtype]
+
+
+# ------------------------------------------------------------------ normalisation
+
+def norm_backward_into(x, dy, L, mean, rstd, w, dx):
+    """The C entry with dx given (it may be dy): dx, dw, db."""
+    N, C, _ = x.shape
+    lib = gtp.lib()
+    n = lib.gtp_layer_norm_backward_work(L, code(x), N, C)
+    work = torch.empty(max(n, 1), dtype=torch.uint8, device="cuda")
+    dw, db = torch.empty((L + 1, C), device="cuda"), torch.empty(C, device="cuda")
+    assert lib.gtp_layer_norm_backward(L, x.data_ptr(), code(x), w.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                       dy.data_ptr(), N, C, dx.data_ptr(), dw.data_ptr(), db.data_ptr(), work.data_ptr(),
+                                       n, stream()) == gtp.GTP_OK
+    return dx, dw, db
+
+
+# rows in a wave, in registers (scalars; degrees), too long for them (degrees; scalars), and the general path (short; long)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,C,L", [(40, 256, 0), (9, 4000, 0), (40, 64, 2), (9, 512, 6), (5, 600, 8), (7, 9000, 0),
+                                   (70, 1, 1), (3, 7, 0), (2, 70001, 0)])
+def test_norm_gradient_in_place(N, C, L, dtype):
+    _say(f"norm gradient in place N={N} C={C} L={L} {dtype}")
+    x, dy, w, b = norm_case(N, C, L, dtype, 6)
+    y, mean, rstd = gtp.gtp_layer_norm(x, L, w, b)
+    want = norm_backward_into(x, dy, L, mean, rstd, w, torch.empty_like(dy))
+    norm_check(x, dy, w, b, L, y, mean, rstd, dict(zip(("dx", "dw", "db"), want)), "apart")
+    z = dy.clone()
+    got = norm_backward_into(x, z, L, mean, rstd, w, z)
+    assert all(torch.equal(g, e) for g, e in zip(got, want))
