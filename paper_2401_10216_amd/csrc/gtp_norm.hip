@@ -834,12 +834,12 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
   return s;
 }
 
-// Any degree and channel count: one workgroup a row, a degree at a time.
+// Any degree and channel count: one workgroup a row, a degree at a time.  y may be x
+// (and dx below dy): an element is read for the last time by the thread that writes it.
 template <typename T>
-__global__ __launch_bounds__(kAnyThreads) void k_norm_any(const T* __restrict__ x, const float* __restrict__ w,
-                                                          const float* __restrict__ b, float eps, int64_t C, int L,
-                                                          T* __restrict__ y, float* __restrict__ mean,
-                                                          float* __restrict__ rstd) {
+__global__ __launch_bounds__(kAnyThreads) void k_norm_any(const T* x, const float* __restrict__ w,
+                                                          const float* __restrict__ b, float eps, int64_t C, int L, T* y,
+                                                          float* __restrict__ mean, float* __restrict__ rstd) {
   __shared__ float red[kAnyThreads / 64];
   lds_poison(red, kAnyThreads / 64);
   const int64_t n = blockIdx.x;
@@ -871,11 +871,10 @@ __global__ __launch_bounds__(kAnyThreads) void k_norm_any(const T* __restrict__ 
 }
 
 template <typename T>
-__global__ __launch_bounds__(kAnyThreads) void k_norm_dx_any(const T* __restrict__ x, const T* __restrict__ dy,
+__global__ __launch_bounds__(kAnyThreads) void k_norm_dx_any(const T* __restrict__ x, const T* dy,
                                                              const float* __restrict__ w,
                                                              const float* __restrict__ mean,
-                                                             const float* __restrict__ rstd, int64_t C, int L,
-                                                             T* __restrict__ dx) {
+                                                             const float* __restrict__ rstd, int64_t C, int L, T* dx) {
   __shared__ float red[kAnyThreads / 64];
   lds_poison(red, kAnyThreads / 64);
   const int64_t n = blockIdx.x;

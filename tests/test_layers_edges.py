@@ -57,3 +57,14 @@ def test_norm_gradient_in_place(N, C, L, dtype):
     z = dy.clone()
     got = norm_backward_into(x, z, L, mean, rstd, w, z)
     assert all(torch.equal(g, e) for g, e in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,C,L", [(40, 256, 0), (9, 4000, 0), (9, 512, 6), (5, 600, 8), (3, 65, 12), (7, 9000, 0),
+                                   (70, 1, 1), (3, 7, 0), (2, 70001, 0)])
+def test_norm_in_place(N, C, L, dtype):
+    x, _, w, b = norm_case(N, C, L, dtype, 7)
+    want = gtp.gtp_layer_norm(x, L, w, b)
+    z = x.clone()
+    got = gtp.gtp_layer_norm(z, L, w, b, y=z)
+    assert got[0].data_ptr() == z.data_ptr() and all(torch.equal(g, e) for g, e in zip(got, want))
