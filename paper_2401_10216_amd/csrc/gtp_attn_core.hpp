@@ -77,8 +77,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {  // to nearest
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 // Two values in three parts.  GUARD: an infinity (and what rounds to it) is its third
-// part alone, which meets no part of the other operand but the first: infinity times
-// that is what the product is, where infinity times a second part of zero would be NaN.
+// part, which meets no part of the other operand but the first: infinity times that is
+// what the product is, where infinity times a second part of zero would be NaN.  Its own
+// first part is 1 of its sign, so that the other operand's third part, too, may be one.
 template <bool GUARD>
 __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&o)[3]) {
   o[0] = pack_bf16(a, b);
@@ -88,7 +89,7 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&o)[3]) {
   if constexpr (GUARD) {
     ia = fabsf(ha) == INFINITY;
     ib = fabsf(hb) == INFINITY;
-    o[0] = (ia ? 0u : o[0] & 0xffffu) | (ib ? 0u : o[0] & 0xffff0000u);
+    o[0] ^= (ia ? 0x4000u : 0u) | (ib ? 0x40000000u : 0u);  // 0x7f80, infinity, to 0x3f80, 1
     ra = ia ? 0.0f : ra;
     rb = ib ? 0.0f : rb;
   }

@@ -68,3 +68,18 @@ def test_norm_in_place(N, C, L, dtype):
     z = x.clone()
     got = gtp.gtp_layer_norm(z, L, w, b, y=z)
     assert got[0].data_ptr() == z.data_ptr() and all(torch.equal(g, e) for g, e in zip(got, want))
+
+
+# ------------------------------------------------------------------ attention: infinities, large values
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d", [4, 72, 200])
+def test_attention_infinity_times_infinity(d, dtype):
+    """Infinity times minus infinity is a score of minus infinity, as a finite number times it is."""
+    c = Case(dtype, [8], [8], 1, 1, d)
+    c.q.fill_(0.25)
+    c.q[3, 0, 1] = math.inf
+    c.k.fill_(0.0)
+    c.k[:, 0, 1] = -math.inf  # every score of every row
+    o, lse = c.forward()
+    assert bool((o == 0).all()) and bool((lse == -math.inf).all())
