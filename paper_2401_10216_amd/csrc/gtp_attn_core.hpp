@@ -76,31 +76,28 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {  // to nearest, ties to even
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
-// Two values in three parts.  GUARD: an infinity (and what rounds to it) is its third
-// part, which meets no part of the other operand but the first: infinity times that is
-// what the product is, where infinity times a second part of zero would be NaN.  Its own
-// first part is 1 of its sign, so that the other operand's third part, too, may be one.
+// Two values in three parts.  GUARD: a value is cut to the largest bf16 value before its
+// first rounding, what that leaves is in the other parts.  An infinity is its third part,
+// which meets no part of the other operand but the first: infinity times that is what the
+// product is, where infinity times a second part of zero would be NaN.  Its own first part
+// is a number of its sign near 1, so that the other operand's third part may be one too.
+// NaN stays in the second and third.
 template <bool GUARD>
 __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&o)[3]) {
-  o[0] = pack_bf16(a, b);
-  float ha = __uint_as_float(o[0] << 16), hb = __uint_as_float(o[0] & 0xffff0000u);
-  float ra = a - ha, rb = b - hb;
-  bool ia = false, ib = false;
+  constexpr float kMost = 0x1.fep127f;  // 0x7f7f
+  if constexpr (GUARD)
+    o[0] = pack_bf16(__builtin_amdgcn_fmed3f(a, -kMost, kMost), __builtin_amdgcn_fmed3f(b, -kMost, kMost));
+  else
+    o[0] = pack_bf16(a, b);
+  const float ra = a - __uint_as_float(o[0] << 16), rb = b - __uint_as_float(o[0] & 0xffff0000u);
   if constexpr (GUARD) {
-    ia = fabsf(ha) == INFINITY;
-    ib = fabsf(hb) == INFINITY;
-    o[0] ^= (ia ? 0x4000u : 0u) | (ib ? 0x40000000u : 0u);  // 0x7f80, infinity, to 0x3f80, 1
-    ra = ia ? 0.0f : ra;
-    rb = ib ? 0.0f : rb;
+    const bool ia = fabsf(a) == INFINITY, ib = fabsf(b) == INFINITY;
+    o[0] ^= (ia ? 0x4000u : 0u) | (ib ? 0x40000000u : 0u);  // 0x7f7f to 0x3f7f
+    o[1] = pack_bf16(ia ? 0.0f : ra, ib ? 0.0f : rb);
+  } else {
+    o[1] = pack_bf16(ra, rb);
   }
-  o[1] = pack_bf16(ra, rb);
-  ra -= __uint_as_float(o[1] << 16);
-  rb -= __uint_as_float(o[1] & 0xffff0000u);
-  if constexpr (GUARD) {
-    ra = ia ? ha : ra;
-    rb = ib ? hb : rb;
-  }
-  o[2] = pack_bf16(ra, rb);
+  o[2] = pack_bf16(ra - __uint_as_float(o[1] << 16), rb - __uint_as_float(o[1] & 0xffff0000u));
 }
 __device__ __forceinline__ f32x16 mfma16(const u32x4& a, const u32x4& b, const f32x16& acc) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0,

@@ -8,7 +8,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from test_layers import BF16, F32, Case, _say, gen, norm_case, norm_check, randn  # noqa: E402,F401
+from test_layers import BF16, C32, F32, Case, _say, close, norm_case, norm_check  # noqa: E402
 from paper_2401_10216_amd import gtp  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -83,3 +83,27 @@ def test_attention_infinity_times_infinity(d, dtype):
     c.k[:, 0, 1] = -math.inf  # every score of every row
     o, lse = c.forward()
     assert bool((o == 0).all()) and bool((lse == -math.inf).all())
+
+
+@pytest.mark.parametrize("d", [4, 72, 200])
+def test_attention_values_near_the_largest(d):
+    """fp32 values above the largest bf16 value (3.39e38) are what they are: a score of such a key with a small enough
+    query is finite, and so are its gradients."""
+    c = Case(F32, [40], [50], 1, 1, d, scale=1.0)
+    c.q.fill_(0.0)
+    c.q[:, 0, 0] = 1.0
+    c.q[:, 0, 1] = 2.0 ** -126
+    c.k[:, 0, 1:] = 0.0
+    c.k[2, 0, 1] = torch.finfo(F32).max
+    c.k[3, 0, 1] = -torch.finfo(F32).max
+    ro, rl, size = c.ref()
+    o, lse = c.forward()
+    # a score's terms are below 4 + 4: P moves by C32 of that, with room for the sums
+    tol = 16 * C32
+    close(o, ro, tol * size + 1e-30, "o")
+    close(lse, rl, tol * torch.ones_like(rl), "lse")
+    g = c.backward(o, lse)
+    for n, (want, terms, e32) in zip(("dq", "dk", "dv"), c.ref((c.do.double(), o.double(), lse.double()))):
+        held = terms < torch.finfo(F32).max  # dq's terms dS k may pass fp32's range, as a product of finite numbers can
+        assert float(held.double().mean()) > 0.5 and (n == "dq" or bool(held.all()))
+        close(g[n][held], want[held], (tol * e32 + 2.0 ** -23 * want.abs() + 1e-30)[held], n)
