@@ -117,6 +117,9 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
     mma_turned<T, DP, BN>(tk, 0, 0, ds, lane, acc);
   }
   if (!there) return;
+  if (lse == -INFINITY)  // an empty row: zeros, whatever k holds (a zero times an infinity would be NaN)
+#pragma unroll
+    for (int i = 0; i < NDT; ++i) acc[i] = zero16();
   if (a.splits > 1) {
     store_columns<float>(part_row(a.part, w.split, a.Tq * a.H, qi * a.H + h, a.d), acc, a.scale, 0, a.d, hi,
                          a.d % 4 == 0);

@@ -107,3 +107,19 @@ def test_attention_values_near_the_largest(d):
         held = terms < torch.finfo(F32).max  # dq's terms dS k may pass fp32's range, as a product of finite numbers can
         assert float(held.double().mean()) > 0.5 and (n == "dq" or bool(held.all()))
         close(g[n][held], want[held], (tol * e32 + 2.0 ** -23 * want.abs() + 1e-30)[held], n)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("ql,kl", [([8], [8]), ([1], [9000])])
+def test_attention_gradient_of_rows_of_minus_infinity(ql, kl, dtype):
+    """A row whose every score is minus infinity has an output of zeros, so no gradient comes from it or to it."""
+    c = Case(dtype, ql, kl, 2, 2, 72)
+    c.q.fill_(1.0)
+    c.k.fill_(0.0)
+    c.k[:, 0, 1] = -math.inf  # the first head's rows; the second's are ordinary
+    o, lse = c.forward()
+    assert bool((o[:, 0] == 0).all()) and bool((lse[:, 0] == -math.inf).all()) and bool(torch.isfinite(lse[:, 1]).all())
+    g = c.backward(o, lse)
+    for n in ("dq", "dk", "dv"):
+        assert not bool(g[n][:, 0].any()), n
+        assert bool(torch.isfinite(g[n]).all()) and (n != "dv" or bool(g[n][:, 1].any())), n
