@@ -22,20 +22,21 @@ namespace {
 // delta[t, h] = sum_i dout[t, h, i] o[t, h, i]: 16 lanes a row.  In a
 // pass of its own, once for both gradients: dout and o read once, HBM's time for the long
 // cases and a launch's (4 us) for the short.
+constexpr uint32_t kDeltaGrid = 1u << 20;  // workgroups at most: a launch holds less than 2^32 threads
 template <typename T>
 __global__ __launch_bounds__(256) void k_attn_delta(const AttnArgs a) {
-  const int64_t n = a.Tq * a.H, id = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4);
+  const int64_t n = a.Tq * a.H;
   const int i0 = threadIdx.x & 15;
-  float s = 0.0f;
-  if (id < n) {
+  for (int64_t id = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4); id < n; id += int64_t(gridDim.x) * 16) {
     const int64_t t = id / a.H, h = id % a.H;
     const T* o = static_cast<const T*>(a.o.p) + t * a.o.row + h * a.o.head;
     const T* g = static_cast<const T*>(a.dout.p) + t * a.dout.row + h * a.dout.head;
+    float s = 0.0f;
     for (int i = i0; i < a.d; i += 16) s = fmaf(to_f32<T>(o[i]), to_f32<T>(g[i]), s);
-  }
 #pragma unroll
-  for (int o = 8; o > 0; o >>= 1) s += __shfl_xor(s, o);
-  if (id < n && i0 == 0) a.delta[id] = s;
+    for (int x = 8; x > 0; x >>= 1) s += __shfl_xor(s, x);  // a row's lanes are in the loop together
+    if (i0 == 0) a.delta[id] = s;
+  }
 }
 
 // Workgroup: 32 NW rows of one key head (a wave 32), keys in tiles of 32.
@@ -150,7 +151,8 @@ hipError_t launch(const AttnArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_attn_delta(const AttnArgs& a, hipStream_t s) {
-  const uint32_t n = uint32_t((a.Tq * a.H + 15) / 16);
+  const int64_t all = (a.Tq * a.H + 15) / 16;
+  const uint32_t n = all < kDeltaGrid ? uint32_t(all) : kDeltaGrid;
   if (a.bf16)
     k_attn_delta<uint16_t><<<n, 256, 0, s>>>(a);
   else

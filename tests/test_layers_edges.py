@@ -123,3 +123,20 @@ def test_attention_gradient_of_rows_of_minus_infinity(ql, kl, dtype):
     for n in ("dq", "dk", "dv"):
         assert not bool(g[n][:, 0].any()), n
         assert bool(torch.isfinite(g[n]).all()) and (n != "dv" or bool(g[n][:, 1].any())), n
+
+
+def test_attention_gradient_of_many_rows_and_heads():
+    """More than 2^28 rows of heads: more threads than one launch holds, 16 a row."""
+    B, nq, nk, H = 16385, 64, 4, 256
+    assert B * nq * H > 1 << 28
+    c = Case(BF16, [nq], [nk], H, 1, 1)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    q, do = (torch.randn((B * nq, H, 1), generator=g, device="cuda", dtype=BF16) for _ in range(2))
+    k, v = (torch.randn((B * nk, 1, 1), generator=g, device="cuda", dtype=BF16) for _ in range(2))
+    o, lse = gtp.gtp_attention(q, k, v, scale=c.scale, max_q=nq, max_k=nk)
+    grads = gtp.gtp_attention_backward(q, k, v, o, do, lse, scale=c.scale, max_q=nq, max_k=nk)
+    for b in (0, 7000, B - 1):
+        rows, keys = slice(b * nq, (b + 1) * nq), slice(b * nk, (b + 1) * nk)
+        c.q, c.k, c.v, c.do = q[rows], k[keys], v[keys], do[rows]
+        c.check_forward(o[rows], lse[rows])
+        c.check_backward(o[rows], lse[rows], {"dq": grads["dq"][rows], "dk": grads["dk"][keys], "dv": grads["dv"][keys]})
