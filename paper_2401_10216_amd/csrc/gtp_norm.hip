@@ -834,38 +834,43 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
   return s;
 }
 
-// Any degree and channel count: one workgroup a row, a degree at a time.  y may be x
-// (and dx below dy): an element is read for the last time by the thread that writes it.
+// Any degree and channel count: one workgroup a row (a channel, in the weights' sums), a
+// degree at a time.  y may be x (and dx below dy): an element is read for the last time by
+// the thread that writes it.
+constexpr int64_t kAnyGrid = 1 << 20;  // workgroups at most: a launch holds less than 2^32 threads
 template <typename T>
 __global__ __launch_bounds__(kAnyThreads) void k_norm_any(const T* x, const float* __restrict__ w,
-                                                          const float* __restrict__ b, float eps, int64_t C, int L, T* y,
-                                                          float* __restrict__ mean, float* __restrict__ rstd) {
+                                                          const float* __restrict__ b, float eps, int64_t N, int64_t C,
+                                                          int L, T* y, float* __restrict__ mean,
+                                                          float* __restrict__ rstd) {
   __shared__ float red[kAnyThreads / 64];
   lds_poison(red, kAnyThreads / 64);
-  const int64_t n = blockIdx.x;
-  const int64_t K = int64_t(L + 1) * (L + 1), base = n * C * K;
-  for (int l = 0; l <= L; ++l) {
-    const int64_t M = 2 * l + 1, cnt = C * M;
-    float mu = 0.0f;
-    if (l == 0) {
+  const int64_t K = int64_t(L + 1) * (L + 1);
+  for (int64_t n = blockIdx.x; n < N; n += gridDim.x) {
+    const int64_t base = n * C * K;
+    for (int l = 0; l <= L; ++l) {
+      const int64_t M = 2 * l + 1, cnt = C * M;
+      float mu = 0.0f;
+      if (l == 0) {
+        float s = 0.0f;
+        for (int64_t c = threadIdx.x; c < C; c += kAnyThreads) s += ld(x, base + c * K);
+        mu = block_sum(s, red) / float(C);
+        if (mean && threadIdx.x == 0) mean[n] = mu;
+      }
       float s = 0.0f;
-      for (int64_t c = threadIdx.x; c < C; c += kAnyThreads) s += ld(x, base + c * K);
-      mu = block_sum(s, red) / float(C);
-      if (mean && threadIdx.x == 0) mean[n] = mu;
-    }
-    float s = 0.0f;
-    for (int64_t q = threadIdx.x; q < cnt; q += kAnyThreads) {
-      const int64_t c = q / M;
-      const float v = ld(x, base + c * K + l * l + (q - c * M)) - mu;
-      s = fmaf(v, v, s);
-    }
-    const float r = 1.0f / sqrtf(block_sum(s, red) / float(cnt) + eps);
-    if (rstd && threadIdx.x == 0) rstd[n * (L + 1) + l] = r;
-    for (int64_t q = threadIdx.x; q < cnt; q += kAnyThreads) {
-      const int64_t c = q / M, i = base + c * K + l * l + (q - c * M);
-      const float v = (ld(x, i) - mu) * r;
-      const float wl = w ? w[l * C + c] : 1.0f;
-      st(y, i, l == 0 && b ? fmaf(v, wl, b[c]) : v * wl);
+      for (int64_t q = threadIdx.x; q < cnt; q += kAnyThreads) {
+        const int64_t c = q / M;
+        const float v = ld(x, base + c * K + l * l + (q - c * M)) - mu;
+        s = fmaf(v, v, s);
+      }
+      const float r = 1.0f / sqrtf(block_sum(s, red) / float(cnt) + eps);
+      if (rstd && threadIdx.x == 0) rstd[n * (L + 1) + l] = r;
+      for (int64_t q = threadIdx.x; q < cnt; q += kAnyThreads) {
+        const int64_t c = q / M, i = base + c * K + l * l + (q - c * M);
+        const float v = (ld(x, i) - mu) * r;
+        const float wl = w ? w[l * C + c] : 1.0f;
+        st(y, i, l == 0 && b ? fmaf(v, wl, b[c]) : v * wl);
+      }
     }
   }
 }
@@ -874,32 +879,35 @@ template <typename T>
 __global__ __launch_bounds__(kAnyThreads) void k_norm_dx_any(const T* __restrict__ x, const T* dy,
                                                              const float* __restrict__ w,
                                                              const float* __restrict__ mean,
-                                                             const float* __restrict__ rstd, int64_t C, int L, T* dx) {
+                                                             const float* __restrict__ rstd, int64_t N, int64_t C,
+                                                             int L, T* dx) {
   __shared__ float red[kAnyThreads / 64];
   lds_poison(red, kAnyThreads / 64);
-  const int64_t n = blockIdx.x;
-  const int64_t K = int64_t(L + 1) * (L + 1), base = n * C * K;
-  for (int l = 0; l <= L; ++l) {
-    const int64_t M = 2 * l + 1, cnt = C * M;
-    const float mu = l == 0 ? mean[n] : 0.0f, r = rstd[n * (L + 1) + l];
-    float sg = 0.0f, sx = 0.0f;
-    for (int64_t q = threadIdx.x; q < cnt; q += kAnyThreads) {
-      const int64_t c = q / M, i = base + c * K + l * l + (q - c * M);
-      const float g = ld(dy, i) * (w ? w[l * C + c] : 1.0f);
-      sg += g;
-      sx = fmaf(g, (ld(x, i) - mu) * r, sx);
-    }
-    sg = l == 0 ? block_sum(sg, red) / float(cnt) : 0.0f;
-    sx = block_sum(sx, red) / float(cnt);
-    for (int64_t q = threadIdx.x; q < cnt; q += kAnyThreads) {
-      const int64_t c = q / M, i = base + c * K + l * l + (q - c * M);
-      const float g = ld(dy, i) * (w ? w[l * C + c] : 1.0f);
-      st(dx, i, r * (g - sg - (ld(x, i) - mu) * r * sx));
+  const int64_t K = int64_t(L + 1) * (L + 1);
+  for (int64_t n = blockIdx.x; n < N; n += gridDim.x) {
+    const int64_t base = n * C * K;
+    for (int l = 0; l <= L; ++l) {
+      const int64_t M = 2 * l + 1, cnt = C * M;
+      const float mu = l == 0 ? mean[n] : 0.0f, r = rstd[n * (L + 1) + l];
+      float sg = 0.0f, sx = 0.0f;
+      for (int64_t q = threadIdx.x; q < cnt; q += kAnyThreads) {
+        const int64_t c = q / M, i = base + c * K + l * l + (q - c * M);
+        const float g = ld(dy, i) * (w ? w[l * C + c] : 1.0f);
+        sg += g;
+        sx = fmaf(g, (ld(x, i) - mu) * r, sx);
+      }
+      sg = l == 0 ? block_sum(sg, red) / float(cnt) : 0.0f;
+      sx = block_sum(sx, red) / float(cnt);
+      for (int64_t q = threadIdx.x; q < cnt; q += kAnyThreads) {
+        const int64_t c = q / M, i = base + c * K + l * l + (q - c * M);
+        const float g = ld(dy, i) * (w ? w[l * C + c] : 1.0f);
+        st(dx, i, r * (g - sg - (ld(x, i) - mu) * r * sx));
+      }
     }
   }
 }
 
-// Partial sums of dw and db over a chunk of rows: workgroup (c, chunk).
+// Partial sums of dw and db over a chunk of rows: workgroup (channels, chunk).
 // partial[chunk][(L + 2) C]: L + 1 rows of dw, then db.
 template <typename T>
 __global__ __launch_bounds__(kAnyThreads) void k_norm_dw_any(const T* __restrict__ x, const T* __restrict__ dy,
@@ -908,29 +916,31 @@ __global__ __launch_bounds__(kAnyThreads) void k_norm_dw_any(const T* __restrict
                                                              int L, int64_t chunk, float* __restrict__ partial) {
   __shared__ float red[kAnyThreads / 64];
   lds_poison(red, kAnyThreads / 64);
-  const int64_t c = blockIdx.x, n0 = int64_t(blockIdx.y) * chunk;
+  const int64_t n0 = int64_t(blockIdx.y) * chunk;
   const int64_t rows = n0 + chunk < N ? chunk : N - n0;
   const int64_t K = int64_t(L + 1) * (L + 1);
-  float* const out = partial + int64_t(blockIdx.y) * (L + 2) * C + c;
-  for (int l = 0; l <= L; ++l) {
-    const int64_t M = 2 * l + 1;
-    float s = 0.0f, sb = 0.0f;
-    for (int64_t q = threadIdx.x; q < rows * M; q += kAnyThreads) {
-      const int64_t r = q / M, n = n0 + r, i = (n * C + c) * K + l * l + (q - r * M);
-      const float d = ld(dy, i);
-      s = fmaf(d, (ld(x, i) - (l == 0 ? mean[n] : 0.0f)) * rstd[n * (L + 1) + l], s);
-      sb += d;
-    }
-    s = block_sum(s, red);
-    if (threadIdx.x == 0) out[l * C] = s;
-    if (l == 0) {
-      sb = block_sum(sb, red);
-      if (threadIdx.x == 0) out[(L + 1) * C] = sb;
+  for (int64_t c = blockIdx.x; c < C; c += gridDim.x) {
+    float* const out = partial + int64_t(blockIdx.y) * (L + 2) * C + c;
+    for (int l = 0; l <= L; ++l) {
+      const int64_t M = 2 * l + 1;
+      float s = 0.0f, sb = 0.0f;
+      for (int64_t q = threadIdx.x; q < rows * M; q += kAnyThreads) {
+        const int64_t r = q / M, n = n0 + r, i = (n * C + c) * K + l * l + (q - r * M);
+        const float d = ld(dy, i);
+        s = fmaf(d, (ld(x, i) - (l == 0 ? mean[n] : 0.0f)) * rstd[n * (L + 1) + l], s);
+        sb += d;
+      }
+      s = block_sum(s, red);
+      if (threadIdx.x == 0) out[l * C] = s;
+      if (l == 0) {
+        sb = block_sum(sb, red);
+        if (threadIdx.x == 0) out[(L + 1) * C] = sb;
+      }
     }
   }
 }
 
-// The parts' sums, added in order: a workgroup takes 16 columns, 64 groups of
+// The parts' sums, added in order: a workgroup takes 16 columns at a time, 64 groups of
 // threads every 64th part each, then a tree over the groups.
 constexpr int kSumThreads = 1024, kSumCols = 16;
 __global__ __launch_bounds__(kSumThreads) void k_norm_sum(const float* __restrict__ partial, int parts, int64_t cols,
@@ -939,31 +949,33 @@ __global__ __launch_bounds__(kSumThreads) void k_norm_sum(const float* __restric
   __shared__ float red[kSumThreads];
   lds_poison(red, kSumThreads);
   const int c = threadIdx.x % kSumCols, g = threadIdx.x / kSumCols;
-  const int64_t col = int64_t(blockIdx.x) * kSumCols + c;
-  float s = 0.0f;
-  if (col < cols) {
+  for (int64_t col0 = int64_t(blockIdx.x) * kSumCols; col0 < cols; col0 += int64_t(gridDim.x) * kSumCols) {
+    const int64_t col = col0 + c;
+    float s = 0.0f;
+    if (col < cols) {
 #pragma unroll 8
-    for (int i = g; i < parts; i += kSumThreads / kSumCols) s += partial[i * cols + col];
-  }
-  red[threadIdx.x] = s;
+      for (int i = g; i < parts; i += kSumThreads / kSumCols) s += partial[i * cols + col];
+    }
+    __syncthreads();  // the columns before are read
+    red[threadIdx.x] = s;
 #pragma unroll
-  for (int o = kSumThreads / 2; o >= kSumCols; o /= 2) {
-    __syncthreads();
-    if (int(threadIdx.x) < o) red[threadIdx.x] += red[threadIdx.x + o];
-  }
-  if (g == 0 && col < cols) {
-    if (col < wcols) {
-      if (dw) dw[col] = red[c];
-    } else if (db) {
-      db[col - wcols] = red[c];
+    for (int o = kSumThreads / 2; o >= kSumCols; o /= 2) {
+      __syncthreads();
+      if (int(threadIdx.x) < o) red[threadIdx.x] += red[threadIdx.x + o];
+    }
+    if (g == 0 && col < cols) {
+      if (col < wcols) {
+        if (dw) dw[col] = red[c];
+      } else if (db) {
+        db[col - wcols] = red[c];
+      }
     }
   }
 }
 
 hipError_t sum_parts(const NormArgs& a, int64_t parts, hipStream_t s) {
-  const int64_t cols = (a.L + 2) * a.C;
-  k_norm_sum<<<dim3{uint32_t((cols + kSumCols - 1) / kSumCols)}, kSumThreads, 0, s>>>(a.partial, int(parts), cols,
-                                                                                     (a.L + 1) * a.C, a.dw, a.db);
+  const int64_t cols = (a.L + 2) * a.C, n = std::min((cols + kSumCols - 1) / kSumCols, kAnyGrid);
+  k_norm_sum<<<dim3{uint32_t(n)}, kSumThreads, 0, s>>>(a.partial, int(parts), cols, (a.L + 1) * a.C, a.dw, a.db);
   return hipGetLastError();
 }
 
@@ -1150,12 +1162,12 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
   if (short_rows(a.L, a.C, a.bf16, wide, &h)) return launch_short(a, false, h, s);
   Lay y;
   if (layout(a.L, a.C, a.bf16, wide, false, &y)) return with_layout(a.bf16, y, Forward{a, y, s});
-  const dim3 grid{uint32_t(a.N)};
+  const dim3 grid{uint32_t(std::min(a.N, kAnyGrid))};
   if (a.bf16)
-    k_norm_any<<<grid, kAnyThreads, 0, s>>>(static_cast<const uint16_t*>(a.x), a.w, a.b, a.eps, a.C, a.L,
+    k_norm_any<<<grid, kAnyThreads, 0, s>>>(static_cast<const uint16_t*>(a.x), a.w, a.b, a.eps, a.N, a.C, a.L,
                                             static_cast<uint16_t*>(a.y), a.mean, a.rstd);
   else
-    k_norm_any<<<grid, kAnyThreads, 0, s>>>(static_cast<const float*>(a.x), a.w, a.b, a.eps, a.C, a.L,
+    k_norm_any<<<grid, kAnyThreads, 0, s>>>(static_cast<const float*>(a.x), a.w, a.b, a.eps, a.N, a.C, a.L,
                                             static_cast<float*>(a.y), a.mean, a.rstd);
   return hipGetLastError();
 }
@@ -1189,7 +1201,7 @@ hipError_t launch_norm_backward(const NormArgs& a, hipStream_t s) {
   }
   const int64_t chunks = any_chunks(a.N), chunk = (a.N + chunks - 1) / chunks;
   const int64_t used = a.N ? (a.N + chunk - 1) / chunk : 0;
-  const dim3 grid{uint32_t(a.N)}, gw{uint32_t(a.C), uint32_t(used)};
+  const dim3 grid{uint32_t(std::min(a.N, kAnyGrid))}, gw{uint32_t(std::min(a.C, kAnyGrid)), uint32_t(used)};
   const bool weights = a.dw || a.db;
   // dw and db before dx, which may be written over dy
   if (a.bf16) {
@@ -1197,14 +1209,15 @@ hipError_t launch_norm_backward(const NormArgs& a, hipStream_t s) {
     if (weights && a.N)
       k_norm_dw_any<<<gw, kAnyThreads, 0, s>>>(x, dy, a.mean_in, a.rstd_in, a.N, a.C, a.L, chunk, a.partial);
     if (a.y && a.N)
-      k_norm_dx_any<<<grid, kAnyThreads, 0, s>>>(x, dy, a.w, a.mean_in, a.rstd_in, a.C, a.L,
+      k_norm_dx_any<<<grid, kAnyThreads, 0, s>>>(x, dy, a.w, a.mean_in, a.rstd_in, a.N, a.C, a.L,
                                                  static_cast<uint16_t*>(a.y));
   } else {
     const auto *x = static_cast<const float*>(a.x), *dy = static_cast<const float*>(a.dy);
     if (weights && a.N)
       k_norm_dw_any<<<gw, kAnyThreads, 0, s>>>(x, dy, a.mean_in, a.rstd_in, a.N, a.C, a.L, chunk, a.partial);
     if (a.y && a.N)
-      k_norm_dx_any<<<grid, kAnyThreads, 0, s>>>(x, dy, a.w, a.mean_in, a.rstd_in, a.C, a.L, static_cast<float*>(a.y));
+      k_norm_dx_any<<<grid, kAnyThreads, 0, s>>>(x, dy, a.w, a.mean_in, a.rstd_in, a.N, a.C, a.L,
+                                                 static_cast<float*>(a.y));
   }
   return weights ? sum_parts(a, used, s) : hipGetLastError();
 }

@@ -70,6 +70,34 @@ def test_norm_in_place(N, C, L, dtype):
     assert got[0].data_ptr() == z.data_ptr() and all(torch.equal(g, e) for g, e in zip(got, want))
 
 
+def test_norm_of_many_short_rows():
+    """More than 2^24 rows on the general path: more workgroups of 256 than one launch holds.  (Weight sums of up to 3072
+    terms a lane with signs at random: some 46 units of the terms' magnitudes, below the 256 of C32.)"""
+    x, dy, w, b = norm_case((1 << 24) + 5, 1, 1, F32, 8)
+    y, mean, rstd = gtp.gtp_layer_norm(x, 1, w, b)
+    grads = gtp.gtp_layer_norm_backward(x, dy, 1, mean, rstd, w)
+    norm_check(x, dy, w, b, 1, y, mean, rstd, grads, "many rows")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_norm_of_many_channels(dtype):
+    """More than 2^25 channels: more workgroups of a channel, or of 16 columns of weight sums, than one launch holds.
+    Values whose statistics and gradients are exact: x = 1, -1, ..., so mean 0, rstd 1 / sqrt(1 + 3)."""
+    C = (1 << 25) + 4
+    c = torch.arange(C, device="cuda")
+    s = 1.0 - 2.0 * (c % 2)
+    x = torch.stack([s, -s]).unsqueeze(-1).to(dtype)
+    dy = torch.stack([(c % 4).float(), torch.ones_like(s)]).unsqueeze(-1).to(dtype)
+    y, mean, rstd = gtp.gtp_layer_norm(x, 0, eps=3.0)
+    assert torch.allclose(mean, torch.zeros_like(mean), atol=1e-6) and torch.allclose(rstd, torch.full_like(rstd, 0.5))
+    assert torch.equal(y, x * 0.5)
+    g = gtp.gtp_layer_norm_backward(x, dy, 0, mean, rstd)
+    # row 0: mean of dy 3 / 2, of dy xh -1 / 4; row 1: 1 and 0
+    want = torch.stack([0.5 * ((c % 4) - 1.5 + 0.25 * 0.5 * s), torch.zeros_like(s)]).unsqueeze(-1)
+    assert float((g["dx"].float() - want).abs().max()) <= (2.0 ** -8 if dtype == BF16 else 1e-6)
+    assert torch.allclose(g["dw"][0], 0.5 * s * ((c % 4) - 1), atol=1e-6) and torch.equal(g["db"], (c % 4) + 1.0)
+
+
 # ------------------------------------------------------------------ attention: infinities, large values
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
