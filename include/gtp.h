@@ -341,7 +341,8 @@ gtp_status gtp_layer_norm_backward(int L, const void *x, gtp_dtype dtype, const 
  * read when the call runs: a graph that is replayed draws anew where they were
  * changed between.  The gradient is the same call on dy, without res.
  * x, res (or NULL), y: [groups, K] of `dtype`; y may be x or res itself, else not
- * overlapping them.  0 <= p < 1.  groups K == 0 is a no-op. */
+ * overlapping them.  0 <= p < 1.  groups K == 0 is a no-op.  GTP_ERR_UNSUPPORTED
+ * above 2^37 - 8192 elements or K = 2^31 - 1. */
 gtp_status gtp_dropout(const void *x, const void *res, gtp_dtype dtype, double p, const uint64_t *rng, int64_t groups,
                        int64_t K, void *y, void *stream);
 

@@ -145,7 +145,8 @@ gtp_status gtp_dropout(const void* x, const void* res, gtp_dtype dtype, double p
   if (!(p >= 0.0 && p < 1.0)) return bad("p must be in [0, 1)");
   int64_t n = 0;
   if (!times(groups, K, &n)) return bad("groups and K must be >= 0 and groups K must fit");
-  if (K > kMaxGrid || n / 8192 >= kMaxGrid) return unsupported("more elements than one launch can hold");
+  // a launch holds less than 2^32 threads: 2^24 workgroups of 256, 8192 elements each
+  if (K > kMaxGrid || n > (int64_t(1) << 37) - 8192) return unsupported("more elements than one launch can hold");
   if (n == 0) return GTP_OK;
   if (!x || !y || !rng) return bad("NULL data pointer");
   const int64_t es = elem_size(dtype);
