@@ -382,7 +382,9 @@ int64_t gtp_attention_work(const gtp_attn *a, int backward);
  * m the factors 0 or 1 / (1 - p) of dropped probabilities.  A row without a
  * present key (or whose every score is -infinity) has o = 0 and lse = -infinity.
  * q, o: [Tq, H, d]; k, v: [Tk, Hk, d]; lse: [Tq, H] fp32.  Any nonnegative strides
- * for inputs; outputs' rows must not overlap each other or an input.  The draws,
+ * for inputs; outputs' rows must not overlap each other or an input (slices of one
+ * buffer, side by side or interleaved, do not; where the strides of two tensors
+ * differ, buffers that reach into each other count as overlapping).  The draws,
  * of the generator of gtp_dropout: the rows of a key head's G = H / Hk query heads
  * count together, R = i G + g for row i of the segment, in blocks of 4 rows x 4
  * keys; block ((b Hk + hk) ceil(max_q G / 4) + R / 4) ceil(max_k / 4) + j / 4 takes

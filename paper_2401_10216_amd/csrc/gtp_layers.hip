@@ -3,6 +3,7 @@
 // dispatch.  Nothing here allocates or throws.
 #include "gtp_layers.hpp"
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 
@@ -184,26 +185,42 @@ bool rows_fine(const gtp_rows* r, int64_t T, int heads, int d, int64_t es, bool 
 
 struct Rows {
   const gtp_rows* r;
-  int64_t T;
-  int heads;
+  int64_t T, heads;
 };
 
 int64_t extent(const Rows& t, int d, int64_t es) {
   return t.T == 0 ? 0 : ((t.T - 1) * t.r->row + (t.heads - 1) * t.r->head + d) * es;
 }
 
-// Whether two strided tensors may share memory: their extents meet, and they are
-// not two column ranges of rows with one stride (slices of a packed tensor).
+// Whether two strided tensors may share memory: their extents meet, they are not two
+// column ranges of rows with one stride (slices of a packed tensor), and, where both
+// strides are the same (a dimension of one index has any), some of their rows meet.
 bool rows_overlap(const Rows& a, const Rows& b, int d, int64_t es) {
   if (!a.r || !b.r || a.T == 0 || b.T == 0 || !a.r->data || !b.r->data) return false;
   if (!overlap({a.r->data, extent(a, d, es)}, {b.r->data, extent(b, d, es)})) return false;
-  const int64_t wa = ((a.heads - 1) * a.r->head + d) * es, wb = ((b.heads - 1) * b.r->head + d) * es;
-  const int64_t row = a.r->row * es;
-  if (a.r->row != b.r->row || wa > row || wb > row) return true;
-  const int64_t x = int64_t(reinterpret_cast<uintptr_t>(a.r->data) % uintptr_t(row));
-  const int64_t y = int64_t(reinterpret_cast<uintptr_t>(b.r->data) % uintptr_t(row));
-  const int64_t ab = (y - x + row) % row;  // where b's columns begin behind a's
-  return !(ab >= wa && ab + wb <= row);
+  const int64_t row = a.T > 1 ? a.r->row : b.T > 1 ? b.r->row : 0;
+  if (b.T > 1 && b.r->row != row) return true;
+  // where b's first element lies behind a's: their extents meet, so it is in their range
+  const int64_t at = (int64_t(reinterpret_cast<uintptr_t>(b.r->data)) - int64_t(reinterpret_cast<uintptr_t>(a.r->data))) / es;
+  const int64_t wa = (a.heads - 1) * a.r->head + d, wb = (b.heads - 1) * b.r->head + d;
+  if (row > 0 && wa <= row && wb <= row) {
+    const int64_t column = (at % row + row) % row;
+    if (column >= wa && column + wb <= row) return false;
+  }
+  const int64_t head = a.heads > 1 ? a.r->head : b.heads > 1 ? b.r->head : 0;
+  if (b.heads > 1 && b.r->head != head) return true;
+  // b's row t', head h' lies at + (t' - t) row + (h' - h) head behind a's row t, head h:
+  // walk the shorter dimension, and find where the other comes nearest
+  const bool by_head = std::max(a.heads, b.heads) <= std::max(a.T, b.T);
+  const int64_t na = by_head ? a.heads : a.T, nb = by_head ? b.heads : b.T, step = by_head ? head : row;
+  const int64_t ma = by_head ? a.T : a.heads, mb = by_head ? b.T : b.heads, other = by_head ? row : head;
+  for (int64_t i = 1 - na; i < nb; ++i) {
+    const int64_t x = at + i * step;
+    const int64_t j0 = std::clamp<int64_t>(other > 0 ? -x / other : 0, 1 - ma, mb - 1);
+    for (int64_t j = std::max(j0 - 1, 1 - ma); j <= std::min(j0 + 1, mb - 1); ++j)
+      if (x + j * other < d && x + j * other > -d) return true;
+  }
+  return false;
 }
 
 bool rows_vec(const gtp_rows* r, int64_t es) {

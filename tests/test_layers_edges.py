@@ -168,3 +168,23 @@ def test_attention_gradient_of_many_rows_and_heads():
         c.q, c.k, c.v, c.do = q[rows], k[keys], v[keys], do[rows]
         c.check_forward(o[rows], lse[rows])
         c.check_backward(o[rows], lse[rows], {"dq": grads["dq"][rows], "dk": grads["dk"][keys], "dv": grads["dv"][keys]})
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d", [64, 75])
+def test_attention_gradients_into_slices_by_head(d, dtype):
+    """q, k, v and their gradients interleaved by head: slices of [T, H, 3, d], and of [H, T, 3, d]."""
+    c = Case(dtype, [33, 64, 90], [33, 64, 90], 4, 4, d)
+    o, lse = c.forward()
+    g = c.backward(o, lse)
+    T = sum(c.ql)
+    for shape, turn in (((T, 4, 3, d), lambda t: t), ((4, T, 3, d), lambda t: t.transpose(0, 1))):
+        buf = torch.zeros(shape, dtype=dtype, device="cuda")
+        q, k, v = (turn(t) for t in buf.unbind(2))
+        q.copy_(c.q), k.copy_(c.k), v.copy_(c.v)
+        out = torch.full_like(buf, 7.0)
+        dq, dk, dv = (turn(t) for t in out.unbind(2))
+        o2, lse2 = gtp.gtp_attention(q, k, v, **c.args)
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+        gtp.gtp_attention_backward(q, k, v, o, c.do, lse, **c.args, dq=dq, dk=dk, dv=dv)
+        assert torch.equal(dq, g["dq"]) and torch.equal(dk, g["dk"]) and torch.equal(dv, g["dv"])

@@ -1,10 +1,14 @@
 """The layers around the product on the CPU: sizes that one launch cannot hold are refused before it, layouts of outputs
 that do not overlap are not, and the plain 64-bit forms of the GPU tests against autograd."""
+import ctypes
+import random
+
 import pytest
 
 torch = pytest.importorskip("torch")
 
-from test_layers_host import INVALID, OK, UNSUPPORTED, at, drop  # noqa: E402,F401
+from test_layers_host import INVALID, OK, UNSUPPORTED, at, attn_desc, drop  # noqa: E402
+from paper_2401_10216_amd import gtp  # noqa: E402
 
 
 def test_dropout_refuses_more_than_a_launch_holds():
@@ -12,3 +16,68 @@ def test_dropout_refuses_more_than_a_launch_holds():
     assert drop(groups=1 << 37, K=1, **far) == UNSUPPORTED
     assert drop(groups=(1 << 37) // 49 + 1, K=49, **far) == UNSUPPORTED
     assert drop(groups=1, K=1 << 31, **far) == UNSUPPORTED
+
+
+# ------------------------------------------------------------------ outputs' layouts
+
+def backward_into(grads, T, H, d):
+    """The attention gradient's checks of (pointer, row, head) outputs, B = 0 segments: nothing is launched."""
+    desc = attn_desc(B=0, H=H, Hk=H, d=d, Tq=T, Tk=T, max_q=T, max_k=T, q_off=at(20), k_off=at(21))
+    ins = [gtp._Rows(at(i), H * d, d) for i in range(5)]
+    outs = [gtp._Rows(*g) for g in grads]
+    status = gtp.lib().gtp_attention_backward(ctypes.byref(desc), *map(ctypes.byref, ins), at(5), *map(ctypes.byref, outs),
+                                              at(6), 1 << 40, None)
+    return status, gtp.lib().gtp_last_error().decode()
+
+
+@pytest.mark.parametrize("T,H,d", [(100, 4, 64), (1, 4, 64), (100, 1, 64), (1, 1, 9), (33, 12, 7)])
+def test_gradients_into_any_slice_of_a_packed_tensor(T, H, d):
+    n = T * H * d
+    for name, strides, step in (("[T, 3, H, d]", (3 * H * d, d), H * d), ("[T, H, 3, d]", (3 * H * d, 3 * d), d),
+                                ("[H, T, 3, d]", (3 * d, 3 * T * d), d), ("[H, 3, T, d]", (d, 3 * T * d), T * d),
+                                ("[3, T, H, d]", (H * d, d), n), ("[3, H, T, d]", (d, T * d), n)):
+        grads = [(at(40) + 4 * i * step, *strides) for i in range(3)]
+        assert backward_into(grads, T, H, d)[0] == OK, name
+        grads[2] = (grads[1][0] + 4 * (d - 1), *strides)
+        assert backward_into(grads, T, H, d) == (INVALID, "two outputs overlap"), name
+
+
+def test_overlaps_are_found_by_their_elements():
+    """Random layouts of one pair of strides, each output's own rows apart: refused where an element is shared, and
+    only there."""
+    r, seen = random.Random(5), [0, 0]
+    for _ in range(3000):
+        T, H, d = r.randint(1, 5), r.randint(1, 4), r.randint(1, 5)
+        inner = d + r.randint(0, 7)
+        if r.random() < 0.5:
+            head, row = inner, inner * (H - 1) + d + r.randint(0, 30)
+        else:
+            row, head = inner, inner * (T - 1) + d + r.randint(0, 30)
+        move = r.randint(-40, 40)
+        own = {t * row + h * head + i for t in range(T) for h in range(H) for i in range(d)}
+        shared = bool(own & {e + move for e in own})
+        grads = [(at(30), row, head), (at(40), row, head), (at(40) + 4 * move, row, head)]
+        status, msg = backward_into(grads, T, H, d)
+        assert (status, shared) in ((OK, False), (INVALID, True)), (T, H, d, row, head, move)
+        seen[shared] += 1
+    assert min(seen) > 300
+
+
+def test_an_output_is_told_from_any_input():
+    """o against keys of another length, whose rows may meet each other (expanded, windows)."""
+    r, seen = random.Random(6), [0, 0]
+    for _ in range(3000):
+        Tq, Tk, H, d = r.choice([1, 1, 3]), r.randint(1, 6), r.randint(1, 3), r.randint(1, 5)
+        head = d + r.randint(0, 6)
+        row = head * (H - 1) + d + r.randint(0, 9)
+        krow = row if Tq > 1 else r.choice([0, 1, d - 1, row, 2 * row])
+        move = r.randint(-60, 60)
+        o = {t * row + h * head + i for t in range(Tq) for h in range(H) for i in range(d)}
+        k = {move + t * krow + h * head + i for t in range(Tk) for h in range(H) for i in range(d)}
+        desc = attn_desc(B=0, H=H, Hk=H, d=d, Tq=Tq, Tk=Tk, max_q=Tq, max_k=Tk)
+        rows = [gtp._Rows(*t) for t in ((at(0), H * d, d), (at(40) + 4 * move, krow, head), (at(2), H * d, d), (at(40), row, head))]
+        status = gtp.lib().gtp_attention(ctypes.byref(desc), *map(ctypes.byref, rows), at(5), at(6), 1 << 40, None)
+        shared = bool(o & k)
+        assert (status, shared) in ((OK, False), (INVALID, True)), (Tq, Tk, H, d, row, head, krow, move)
+        seen[shared] += 1
+    assert min(seen) > 300
