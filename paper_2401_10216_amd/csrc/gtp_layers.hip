@@ -244,6 +244,8 @@ gtp_status attn_sizes(const gtp_attn* a, gtp::AttnArgs* g) {
   int64_t n = 0;
   if (!times(a->Tq, int64_t(a->H) * a->d, &n) || !times(a->Tk, int64_t(a->Hk) * a->d, &n))
     return bad("the tensors' sizes must fit");
+  // the parts of a split call: 2 x 128 of fp32 for dk and dv
+  if (n > kMaxElems >> 10) return unsupported("more rows than the work's size can count");
   // workgroups, counted generously: 32 rows or keys each
   const int64_t G = a->H / a->Hk;
   int64_t w = 0;

@@ -81,3 +81,16 @@ def test_an_output_is_told_from_any_input():
         assert (status, shared) in ((OK, False), (INVALID, True)), (Tq, Tk, H, d, row, head, krow, move)
         seen[shared] += 1
     assert min(seen) > 300
+
+
+# ------------------------------------------------------------------ descriptions at the edge of what fits
+
+def test_attention_work_size_fits():
+    """Expanded keys (a row stride of 0) of any number: the size is right or refused, never wrapped."""
+    for shift in range(30, 62):
+        desc = attn_desc(B=1, H=1, Hk=1, d=4, Tq=1 << 20, Tk=1 << shift, max_q=1 << 20, max_k=64)
+        n = gtp.lib().gtp_attention_work(ctypes.byref(desc), 1)
+        assert n == -1 or n >= 4 << 20, shift
+        desc = attn_desc(B=1, H=1, Hk=1, d=4, Tq=1 << 20, Tk=1 << shift, max_q=1 << 20, max_k=1)
+        few = gtp.lib().gtp_attention_work(ctypes.byref(desc), 1)
+        assert (few == -1) == (n == -1) and (few == -1 or few >= (4 << 20) + (32 << shift)), shift
