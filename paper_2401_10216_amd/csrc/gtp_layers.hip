@@ -239,7 +239,8 @@ gtp_status attn_sizes(const gtp_attn* a, gtp::AttnArgs* g) {
   if (!a->k_off && (!times(a->B, a->max_k, &t) || t != a->Tk)) return bad("without k_off, Tk must be B max_k");
   if (a->max_q > a->Tq || a->max_k > a->Tk) return bad("max_q and max_k must not exceed Tq and Tk");
   if (!aligned(a->q_off, 8) || !aligned(a->k_off, 8)) return bad("misaligned pointer");
-  if (!std::isfinite(a->scale)) return bad("scale must be finite");
+  const float scale2 = a->scale * 1.4426950408889634f;  // in units of log 2
+  if (!std::isfinite(a->scale) || !std::isfinite(scale2)) return bad("scale must be finite, times log2(e) too");
   if (!(a->p >= 0.0 && a->p < 1.0)) return bad("p must be in [0, 1)");
   int64_t n = 0;
   if (!times(a->Tq, int64_t(a->H) * a->d, &n) || !times(a->Tk, int64_t(a->Hk) * a->d, &n))
@@ -271,7 +272,7 @@ gtp_status attn_sizes(const gtp_attn* a, gtp::AttnArgs* g) {
   g->d = a->d;
   g->splits = 1;
   g->scale = a->scale;
-  g->scale2 = a->scale * 1.4426950408889634f;
+  g->scale2 = scale2;
   g->threshold = th;
   g->keep = gtp::drop_scale(th);
   g->bf16 = a->dtype == GTP_BF16;

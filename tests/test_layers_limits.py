@@ -85,6 +85,13 @@ def test_an_output_is_told_from_any_input():
 
 # ------------------------------------------------------------------ descriptions at the edge of what fits
 
+def test_attention_refuses_a_scale_that_overflows_in_units_of_log_2():
+    for scale in (3e38, -2.4e38):
+        desc = attn_desc(scale=scale)
+        assert gtp.lib().gtp_attention_work(ctypes.byref(desc), 0) == -1
+    assert gtp.lib().gtp_attention_work(ctypes.byref(attn_desc(scale=2.3e38)), 0) >= 0
+
+
 def test_attention_work_size_fits():
     """Expanded keys (a row stride of 0) of any number: the size is right or refused, never wrapped."""
     for shift in range(30, 62):
