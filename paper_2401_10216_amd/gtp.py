@@ -144,8 +144,11 @@ def _check(status: int, L=None):
 def _stream(stream=None):
     import torch
     if stream is None and torch.cuda.is_initialized():
-        # the current stream's handle without a Stream object around it (several us a call)
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+        # the current stream's handle without a Stream object around it (several us a call), where torch has that
+        # function: its name is not one that torch promises
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return ctypes.c_void_p(raw(torch.cuda.current_device()))
     s = stream if stream is not None else torch.cuda.current_stream()
     return ctypes.c_void_p(s.cuda_stream)
 
@@ -494,26 +497,14 @@ def gtp_sh_filter(L: int, r, h=None, out=None, stream=None):
     return out
 
 
-class _on_stream:
-    """Allocations for a launch on `stream`: memory that the allocator hands out for a stream is free of that
-    stream's earlier work only, so what a call on another stream than the current one writes is allocated for it."""
-
-    def __init__(self, stream):
-        import torch
-        self.ctx = torch.cuda.stream(stream)
-
-    def __enter__(self):
-        self.ctx.__enter__()
-
-    def __exit__(self, *exc):
-        return self.ctx.__exit__(*exc)
-
-
 _HERE = contextlib.nullcontext()
 
 
 def _allocating(stream):
-    return _HERE if stream is None else _on_stream(stream)
+    """Allocations for a launch on `stream`: memory that the allocator hands out for a stream is free of that
+    stream's earlier work only, so what a call on another stream than the current one writes is allocated for it."""
+    import torch
+    return _HERE if stream is None else torch.cuda.stream(stream)
 
 
 def _opt(t, name, shape, dtypes, device):

@@ -101,3 +101,17 @@ def test_attention_work_size_fits():
         desc = attn_desc(B=1, H=1, Hk=1, d=4, Tq=1 << 20, Tk=1 << shift, max_q=1 << 20, max_k=1)
         few = gtp.lib().gtp_attention_work(ctypes.byref(desc), 1)
         assert (few == -1) == (n == -1) and (few == -1 or few >= (4 << 20) + (32 << shift)), shift
+
+
+# ------------------------------------------------------------------ the binding
+
+def test_current_stream_without_the_short_way(monkeypatch):
+    """The current stream's handle where torch lacks the function that gives it without an object."""
+    class Fake:
+        cuda_stream = 77
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Fake())
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.delattr(torch._C, "_cuda_getDevice", raising=False)
+    assert gtp._stream().value == 77 and gtp._stream(Fake()).value == 77
