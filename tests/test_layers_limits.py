@@ -1,12 +1,15 @@
 """The layers around the product on the CPU: sizes that one launch cannot hold are refused before it, layouts of outputs
 that do not overlap are not, and the plain 64-bit forms of the GPU tests against autograd."""
 import ctypes
+import itertools
+import math
 import random
 
 import pytest
 
 torch = pytest.importorskip("torch")
 
+import layers_ref as R  # noqa: E402
 from test_layers_host import INVALID, OK, UNSUPPORTED, at, attn_desc, drop  # noqa: E402
 from paper_2401_10216_amd import gtp  # noqa: E402
 
@@ -115,3 +118,84 @@ def test_current_stream_without_the_short_way(monkeypatch):
     monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
     monkeypatch.delattr(torch._C, "_cuda_getDevice", raising=False)
     assert gtp._stream().value == 77 and gtp._stream(Fake()).value == 77
+
+
+# ------------------------------------------------------------------ the plain 64-bit forms against autograd
+
+def randn64(g, *shape):
+    return torch.randn(shape, generator=g, dtype=torch.float64)
+
+
+@pytest.mark.parametrize("N,C,L", [(1, 1, 0), (5, 7, 0), (4, 1, 1), (3, 6, 2), (2, 3, 5)])
+@pytest.mark.parametrize("weights", [True, False])
+def test_plain_norm_against_autograd(N, C, L, weights):
+    """The forward against one written coefficient by coefficient, the gradient against its derivative."""
+    g = torch.Generator().manual_seed(N + C + L)
+    x, dy = randn64(g, N, C, (L + 1) ** 2), randn64(g, N, C, (L + 1) ** 2)
+    x[..., 0] += 0.5
+    w, b = (randn64(g, L + 1, C), randn64(g, C)) if weights else (None, None)
+    leaves = [t.requires_grad_() for t in (x, w, b) if t is not None]
+    rows = []
+    for n in range(N):
+        mu = sum(x[n, c, 0] for c in range(C)) / C
+        out = []
+        for l in range(L + 1):
+            a = [[x[n, c, k] - (mu if k == 0 else 0.0) for k in range(l * l, (l + 1) ** 2)] for c in range(C)]
+            v = sum(e * e for r in a for e in r) / (C * (2 * l + 1))
+            out.append(torch.stack([torch.stack(r) / (v + 1e-5).sqrt() * (1.0 if w is None else w[l, c]) +
+                                    (b[c] if b is not None and l == 0 else 0.0) for c, r in enumerate(a)]))
+        rows.append(torch.cat(out, 1))
+    want = torch.stack(rows)
+    y, mean, rstd = R.norm(x.detach(), L, *(None if t is None else t.detach() for t in (w, b)), 1e-5)
+    assert torch.allclose(y, want, rtol=1e-12, atol=1e-12)
+    grads = torch.autograd.grad((want * dy).sum(), leaves)
+    dx, dw, db, sw, sb = R.norm_backward(x.detach(), dy, L, None if w is None else w.detach(), mean, rstd)
+    # one channel at degree 0 is its own mean: a gradient of zero, out of terms of rstd = 1 / sqrt(eps)
+    size = float(rstd.max())
+    assert torch.allclose(dx, grads[0], rtol=1e-10, atol=1e-10 * size)
+    if weights:
+        assert torch.allclose(dw, grads[1], rtol=1e-10, atol=1e-10) and torch.allclose(db, grads[2], rtol=1e-10, atol=1e-10)
+    assert bool((sw >= dw.abs() - 1e-12).all()) and bool((sb >= db.abs() - 1e-12).all())
+
+
+@pytest.mark.parametrize("H,Hk,masked,p", [(1, 1, 0, 0.0), (4, 2, 0, 0.0), (6, 2, 0.4, 0.0), (4, 4, 0, 0.3), (4, 1, 0.3, 0.2)])
+def test_plain_attention_against_autograd(H, Hk, masked, p):
+    """One query row at a time, every key of every segment with a factor of 0 or 1 for belonging to it, against the form
+    by segments; the gradient against its derivative."""
+    g = torch.Generator().manual_seed(H + 10 * Hk)
+    ql, kl, d, G = [3, 0, 5, 2], [4, 6, 7, 0], 6, H // Hk
+    qo, ko = ([0, *itertools.accumulate(n)] for n in (ql, kl))
+    q, k, v = (randn64(g, sum(n), h, d).requires_grad_() for n, h in ((ql, H), (kl, Hk), (kl, Hk)))
+    do = randn64(g, sum(ql), H, d)
+    mask = (torch.rand(sum(kl), generator=g) >= masked).to(torch.uint8) if masked else None
+    rng, scale = (12345, 3), 0.7
+    outs, lses = [], []
+    for b in range(len(ql)):
+        for i in range(ql[b]):
+            for h in range(H):
+                there = torch.zeros(sum(kl), dtype=torch.bool)
+                there[ko[b]:ko[b + 1]] = True
+                if mask is not None:
+                    there &= mask.bool()
+                if not bool(there.any()):
+                    outs.append(torch.zeros(d, dtype=torch.float64))
+                    lses.append(torch.tensor(-math.inf, dtype=torch.float64))
+                    continue
+                e = torch.exp((k[:, h // G] * q[qo[b] + i, h]).sum(1) * scale) * there
+                keep = torch.ones(sum(kl), dtype=torch.float64)
+                if p:
+                    full = R.keep_attention(b, h // G, ql[b], kl[b], max(ql), max(kl), G, Hk, p, *rng)
+                    keep[ko[b]:ko[b + 1]] = torch.from_numpy(full[i * G + h % G]).double() * 65536 / (65536 - R.threshold(p))
+                outs.append((e * keep / e.sum()) @ v[:, h // G])
+                lses.append(e.sum().log())
+    want, wl = torch.stack(outs).view(sum(ql), H, d), torch.stack(lses).view(sum(ql), H)
+    grads = torch.autograd.grad((want * do).sum(), (q, k, v))
+    args = (scale, list(zip(qo, qo[1:])), list(zip(ko, ko[1:])), mask, p, rng, max(ql), max(kl))
+    t = [x.detach() for x in (q, k, v)]
+    o, lse, size = R.attention(*t, *args)
+    assert torch.allclose(o, want, rtol=1e-11, atol=1e-12) and torch.equal(torch.isinf(lse), torch.isinf(wl))
+    ok = ~torch.isinf(wl)
+    assert torch.allclose(lse[ok], wl[ok], rtol=1e-11, atol=1e-12) and bool((size >= o.abs() - 1e-12).all())
+    for (got, a, c), e in zip(R.attention(*t, *args, (do, o, lse)), grads):
+        assert torch.allclose(got, e, rtol=1e-10, atol=1e-11)
+        assert bool((a >= got.abs() - 1e-12).all()) and bool((c >= got.abs() - 1e-12).all())
