@@ -310,8 +310,8 @@ gtp_status gtp_sh_filter(int L, const float *r, const float *h, int64_t B, int64
  * L = 0 is the ordinary layer norm over C channels.  w: [L+1, C] fp32 or NULL
  * (ones); b: [C] fp32 or NULL (zeros); eps > 0; y: like x, may be x itself, else
  * not overlapping it; mean: [N] and rstd: [N, L+1] fp32, what the backward
- * reads, or NULL.  0 <= L <= 64; N C == 0 is a no-op.  GTP_ERR_UNSUPPORTED above
- * 2^31 - 1 rows or channels. */
+ * reads, or NULL.  0 <= L <= 64; N C == 0 is a no-op.  GTP_ERR_UNSUPPORTED where N
+ * or (L + 2) C is above 2^31 - 1. */
 gtp_status gtp_layer_norm(int L, const void *x, gtp_dtype dtype, const float *w, const float *b, float eps, int64_t N,
                           int64_t C, void *y, float *mean, float *rstd, void *stream);
 
@@ -390,7 +390,12 @@ int64_t gtp_attention_work(const gtp_attn *a, int backward);
  * keys; block ((b Hk + hk) ceil(max_q G / 4) + R / 4) ceil(max_k / 4) + j / 4 takes
  * calls 2 block (its first two rows) and 2 block + 1, element (R, j) halfword
  * 4 (R mod 2) + j mod 4.  Sums are fp32; with bf16 inputs P and (in the backward)
- * the scores' gradients enter the matrix products rounded to bf16. */
+ * the scores' gradients enter the matrix products rounded to bf16.  What leaves
+ * fp32's range: with fp32 inputs a product of q and k elements above 2^136 may make
+ * its score NaN, whatever its sign; and values of v above 2^120 / (the number of keys) their
+ * sum infinite before it is divided by the row's sum.  GTP_ERR_UNSUPPORTED for heads
+ * longer than 256 and where rows, heads and segments are more than a launch holds
+ * (some 2^25 tiles of 32 rows of a head, or keys of two). */
 gtp_status gtp_attention(const gtp_attn *a, const gtp_rows *q, const gtp_rows *k, const gtp_rows *v, const gtp_rows *o,
                          float *lse, void *work, int64_t work_bytes, void *stream);
 
@@ -400,7 +405,8 @@ gtp_status gtp_attention(const gtp_attn *a, const gtp_rows *q, const gtp_rows *k
  *   dq = scale dS k,  dk = scale dS^T q,  dv = (m P)^T dout,
  * dk and dv summed over the query heads of a key head.  o, lse: as gtp_attention
  * wrote them.  dq, or dk and dv, may be NULL (not computed).  Absent keys have
- * zero gradients.  GTP_ERR_INVALID_ARG where only one of dk and dv is NULL. */
+ * zero gradients, and so do rows with lse = -infinity, which add none to dk and dv.
+ * GTP_ERR_INVALID_ARG where only one of dk and dv is NULL. */
 gtp_status gtp_attention_backward(const gtp_attn *a, const gtp_rows *q, const gtp_rows *k, const gtp_rows *v,
                                   const gtp_rows *o, const gtp_rows *dout, const float *lse, const gtp_rows *dq,
                                   const gtp_rows *dk, const gtp_rows *dv, void *work, int64_t work_bytes, void *stream);

@@ -563,7 +563,9 @@ struct Drop {
 
 // Waves a SIMD that a kernel's registers are cut for: two hide each other's
 // waits (one issues vector instructions while the matrix unit works for the
-// other), where rows, accumulators and a prefetched tile fit 256 registers.
+// other), where rows, accumulators and a prefetched tile of a four-wave workgroup fit
+// 256 registers.  (Two-wave workgroups stage twice as much a lane: fp32 heads of 33-64
+// keep 24 bytes a lane in scratch memory there, 116 with draws.)
 template <typename T, int DP>
 constexpr int waves_per_simd() {
   return DP * int(sizeof(T)) <= 256 ? 2 : 1;

@@ -6,11 +6,13 @@
 // no more and no atomics.
 //
 // A wave's 32 keys are the columns of its products, their k and v in registers, both
-// accumulators too; rows of q and dout are staged for all waves.  The matrix unit bounds
-// the long cases (8 d flops a row and key) as far as registers let two waves a SIMD
-// overlap: two segments of 5000-6500 rows, 16 heads of 64 over 4, bf16, dropped: 1320 us
-// (866 without dropping); 4001 rows, 8 heads of 100, fp32, one wave a SIMD: 787-849 us,
-// 121-130 TFLOP/s.
+// accumulators too; rows of q and dout are staged for all waves.  The registers bound the
+// long cases (8 d flops a row and key): two segments of 5000-6500 rows, 16 heads of 64 over
+// 4, bf16, two waves a SIMD: 821-866 us, dropped 1300-1320; 4001 rows, 8 heads of 100, fp32,
+// one wave a SIMD: 787-849 us, 121-130 TFLOP/s, matrix unit busy 42 % of the cycles, vector
+// unit 33 %; 8192 rows, 8 heads of 128, bf16: 911-946 us, 581-604 TFLOP/s, matrix and vector
+// unit 25 % each: two waves a SIMD cost it the tile ahead and 104 bytes a lane in scratch
+// memory (heads of 97-128 on two-wave workgroups 140, of 65-96 there 80).
 #include "gtp_attn_core.hpp"
 
 namespace gtp {

@@ -9,11 +9,15 @@
 // The rows lie as in the forward: a wave's 32 rows are the columns of its products,
 // their q and dout in registers, keys and values staged for all waves.  dq and dk, dv
 // each make S and dP for themselves: one kernel for all three would add to one of them
-// with atomics, whose order changes the result.  The matrix unit bounds the long cases
-// (6 d flops a row and key), with waits of the one wave a SIMD that fp32 heads longer
-// than 64 leave room for; where probabilities are dropped, the draws add vector work of
-// more than half of that (two segments of 5000-6500 rows, 16 heads of 64 over 4, bf16: 1028 us
-// with, 634 without).  4001 rows, 8 heads of 100, fp32: 624-664 us, 116-123 TFLOP/s.
+// with atomics, whose order changes the result.  The long cases (6 d flops a row and key)
+// wait for matrix and vector unit by turns: fp32 heads longer than 64 leave room for one
+// wave a SIMD.  4001 rows, 8 heads of 100, fp32: 622-664 us, 116-123 TFLOP/s, matrix unit
+// busy 39 % of the cycles, vector unit 32 %; 8192 rows, 8 heads of 128, bf16: 440-472 us,
+// 873-937 TFLOP/s, 39 % and 35 %.  Where probabilities are dropped, the draws add vector work
+// of more than half of that (two segments of 5000-6500 rows, 16 heads of 64 over 4, bf16:
+// 1028-1108 us with, 634-688 without).  fp32 heads above 128 keep 344 bytes a lane in scratch
+// memory (193-256: 712; on two-wave workgroups 908 and 1120) although their rows stay
+// unsplit: 4001 rows, 4 heads of 200, both gradients 2883 us (bf16: 690).
 #include "gtp_attn_core.hpp"
 
 namespace gtp {

@@ -9,17 +9,26 @@
 // themselves are; fp32: in three parts, below an fp32 rounding), their sum l is of the
 // unrounded ones in fp32.
 //
-// Long segments: the matrix unit bounds it (4 d flops a row and key), beside it the
-// exponentials and the operands' way through LDS.  A workgroup's four waves share the
-// staged keys and values, each for 32 rows, so a staged tile is used 128 times; two
-// waves a SIMD, one with vector instructions while the other's products run.  8192
-// rows, 8 heads of 128, bf16: 330-370 us, 740-830 TFLOP/s (library products of that
-// type here: 1200); 4096 rows, 8 heads of 128, fp32: 461-471 us, 146-149 TFLOP/s (154).
+// Long segments: a workgroup's four waves share the staged keys and values, each for 32
+// rows, so a staged tile is used 128 times; two waves a SIMD, one with vector
+// instructions (exponentials, rounding, the row's statistics) while the other's products
+// run.  In bf16 the vector unit is the busier: 8192 rows, 8 heads of 128: 328-372 us,
+// 740-838 TFLOP/s (library products of that type here: 1200), vector unit busy 41 % of the
+// cycles, matrix unit 35 %, LDS bank conflicts in 26 %; two segments of 5000-6500 rows, 16
+// heads of 64 over 4, with as many exponentials for half the products: 594-629 us, 440-463
+// TFLOP/s, vector unit 56 %, matrix unit 25 %; with dropped probabilities 1094 us, of which
+// the draws are 480 (8 heads of 128: 531).  fp32, 4096 rows, 8 heads of 128: 425-471 us,
+// 146-162 TFLOP/s (library products: 154).
 // Few rows: the keys' way from HBM bounds it, so they are dealt to parts, in workgroups of
-// 64 rows, four a CU; one row of 8 heads of 128 against 60000 keys, bf16: 57-62 us, 4.0-4.3
-// TB/s.
+// 64 rows, four a CU; one row of 8 heads of 128 against 60000 keys, bf16: 57-63 us, 3.9-4.3
+// TB/s.  In fp32 it does not get there: 8 rows of 8 heads of 100 against 7000-8001 keys 522
+// us, 0.7 TB/s (bf16: 62 us, 3.1).  The staging registers double with half the threads, and
+// heads of 97-128 keep 348 bytes a lane in scratch memory (heads of 65-96: 216; bf16 heads of
+// 97-128: 68); and of the two waves one works on rows that are not there.
 // Molecules of 5 to 49 atoms: one short pass, waits one after the other (offsets, rows,
-// keys, products): 64 of them, 8 heads of 72, fp32: 21.6 us.
+// keys, products), on that two-wave form: 64 of them, 8 heads of 72, fp32: 21.4-22.8 us.
+// Heads above 128 fill the registers with one wave a SIMD, fp32 ones spill (372 bytes a lane
+// at 193-256): 4001 rows, 4 heads of 200: bf16 176 us, 291 TFLOP/s, fp32 730 us, 70.
 #include <cmath>
 
 #include "gtp_attn_core.hpp"

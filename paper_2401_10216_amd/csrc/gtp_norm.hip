@@ -14,9 +14,16 @@
 // kept in registers between its sums and its results.  A workgroup takes a row at a
 // time, 1 to 16 waves by its length; the sums of a degree go through LDS.  Measured:
 // 16384 x 128 channels of degree 6, fp32, 156-164 us forward (5.0-5.3 TB/s; the chip's
-// best copy 5.5) and 245-260 backward; 65536 rows of 256, 20 and 31 us.  Degree 16 with
-// 64 channels (18496 elements a row, bf16) runs at 200 us forward (3.0 TB/s) and 440-463
-// backward (2.0): its one workgroup a CU cannot load a row while it sums another.
+// best copy 5.5) and 245-263 backward; 65536 rows of 256, 20 and 31 us.
+//
+// Degree 16 with 64 channels (18496 elements a row, bf16, 8192 rows) runs at 200 us
+// forward (3.0 TB/s) and 440-465 backward (2.0): one workgroup a CU cannot load a row
+// while it sums another.  Registers allow no second one forward (ten waves of 126); the
+// backward's sums of dw by element, 83 of its 103 KB of LDS, do not either, and it keeps
+// 56 bytes a lane in scratch memory.  Rows of more than some 24500 elements (forward:
+// 32768) do not stay in registers: 4096 rows of degree 16 with 128 channels, as many
+// bytes, take 288 us forward and 492 backward (dx 329, a kernel of its own for dw 159).
+// Degrees share no sum, so a row could be dealt to workgroups by degrees.
 #include <algorithm>
 #include <type_traits>
 
@@ -240,7 +247,8 @@ __device__ __forceinline__ int elements_of(int R, int V, int AV, int t) {
 }
 
 // Forward.  NI > 0: a row of NI steps stays in registers between its sums and its
-// results (one read); NI = 0: longer rows, read twice.  Degree 0 is summed about
+// results (one read); NI = 0: longer rows, read again for the squares at degree 0 about
+// a thread's mean and for the results.  Degree 0 is summed about
 // each thread's own mean, the threads' means and sums then joined, so a mean far
 // from zero costs no digits.
 template <typename T, int V, int NI, bool K1, bool EVEN>
