@@ -648,9 +648,8 @@ def _attn(q, k, v, scale, q_off, k_off, max_q, max_k, key_mask, p, rng):
             raise ValueError("q_off and k_off must have one length")
         B = off.shape[0] - 1
     if B is None:
-        # equal segments: of max_q and max_k rows, or one of all rows
-        n, most = (Tq, max_q) if max_q is not None else (Tk, max_k)
-        B = 1 if most is None else (n // most if most else 1)
+        # equal segments: of max_q and max_k rows (a side that has any tells how many), or one of all rows
+        B = next((n // most for n, most in ((Tq, max_q), (Tk, max_k)) if n and most), 1)
     max_q = (Tq if q_off is not None else Tq // max(B, 1)) if max_q is None else int(max_q)
     max_k = (Tk if k_off is not None else Tk // max(B, 1)) if max_k is None else int(max_k)
     i64 = (torch.int64,)

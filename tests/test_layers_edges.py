@@ -188,3 +188,16 @@ def test_attention_gradients_into_slices_by_head(d, dtype):
         assert torch.equal(o, o2) and torch.equal(lse, lse2)
         gtp.gtp_attention_backward(q, k, v, o, c.do, lse, **c.args, dq=dq, dk=dk, dv=dv)
         assert torch.equal(dq, g["dq"]) and torch.equal(dk, g["dk"]) and torch.equal(dv, g["dv"])
+
+
+def test_attention_of_no_rows_against_equal_segments():
+    """No query row, three segments of keys: gradients of zero; no key, three segments of rows: outputs of zero."""
+    c = Case(F32, [5], [12], 2, 2, 8)
+    q, do = c.q[:0], c.do[:0]
+    o, lse = gtp.gtp_attention(q, c.k, c.v, max_q=0, max_k=4)
+    g = gtp.gtp_attention_backward(q, c.k, c.v, o, do, lse, max_q=0, max_k=4)
+    assert o.shape == q.shape and not bool(g["dk"].any()) and not bool(g["dv"].any())
+    q, do, k = c.k, c.v, c.q[:0]
+    o, lse = gtp.gtp_attention(q, k, k, max_q=4, max_k=0)
+    g = gtp.gtp_attention_backward(q, k, k, o, do, lse, max_q=4, max_k=0)
+    assert not bool(o.any()) and bool((lse == -math.inf).all()) and not bool(g["dq"].any()) and g["dk"].shape == k.shape

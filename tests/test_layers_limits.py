@@ -108,6 +108,18 @@ def test_attention_work_size_fits():
 
 # ------------------------------------------------------------------ the binding
 
+@pytest.mark.parametrize("Tq,Tk,max_q,max_k,B", [
+    (0, 12, 0, 12, 1), (0, 12, 0, 4, 3), (0, 12, 0, None, 1), (0, 12, 5, 12, 1), (12, 0, 4, 0, 3), (12, 0, None, 0, 1),
+    (0, 0, 0, 0, 1), (0, 0, None, None, 1), (6, 9, 2, None, 3), (6, 9, None, 3, 3), (6, 9, None, None, 1)])
+def test_equal_segments_of_no_rows_on_one_side(Tq, Tk, max_q, max_k, B):
+    """Without offsets the number of segments comes from the side that has rows."""
+    q, k = torch.zeros(Tq, 2, 8), torch.zeros(Tk, 2, 8)
+    desc, _ = gtp._attn(q, k, k, None, None, None, max_q, max_k, None, 0.0, None)
+    assert desc[4] == B and desc[4] * desc[7] == Tq and desc[4] * desc[8] == Tk
+    a = gtp._Attn(*desc)
+    assert gtp.lib().gtp_attention_work(ctypes.byref(a), 0) == 0
+
+
 def test_current_stream_without_the_short_way(monkeypatch):
     """The current stream's handle where torch lacks the function that gives it without an object."""
     class Fake:
