@@ -289,7 +289,7 @@ gtp_status gtp_sh_filter(int L, const float *r, const float *h, int64_t B, int64
                          void *stream);
 
 /* ---- The layers around the product -------------------------------------
- * Normalisation, dropout and attention of a block that holds Gaunt products.
+ * Normalisation, residual steps, dropout and attention of a block that holds Gaunt products.
  * Each commutes with rotations of the SH features: the normalisation scales a
  * degree as a whole, dropout drops a channel as a whole, and attention takes
  * dot products of whole heads, which a rotation leaves alone.
@@ -329,6 +329,62 @@ int64_t gtp_layer_norm_backward_work(int L, gtp_dtype dtype, int64_t N, int64_t 
 gtp_status gtp_layer_norm_backward(int L, const void *x, gtp_dtype dtype, const float *w, const float *mean,
                                    const float *rstd, const void *dy, int64_t N, int64_t C, void *dx, float *dw,
                                    float *db, void *work, int64_t work_bytes, void *stream);
+
+/* The residual step between two parts of a block, with the norms around it: the
+ * part's output a is normalised by degree (post = 1; or left as it is), scaled
+ * per degree and channel and by a gate per channel, added to the residual stream
+ * x, and the sum normalised for the next part:
+ *   t = norm(a) w_post[l, c] + b_post[c] [l = 0]   (post = 0: t = a),
+ *   r = x + scale[l, c] sigmoid(gate[n, c]) t,
+ *   h = norm(r) w_pre[l, c] + b_pre[c] [l = 0],
+ * norm as in gtp_layer_norm (statistics of r before its rounding).  A gate is one
+ * number for all (L+1)^2 coefficients of a channel, so the step commutes with
+ * rotations. */
+typedef struct {
+  int L;                            /* 0..64 */
+  gtp_dtype dtype;                  /* of x, a, gate, r, h and their gradients */
+  int64_t N, C;                     /* rows, channels; GTP_ERR_UNSUPPORTED as in gtp_layer_norm */
+  int post;                         /* 0 or 1 */
+  float eps;                        /* of both norms, positive */
+  const float *scale;               /* [L+1, C] or NULL (ones) */
+  const float *w_post, *b_post;     /* [L+1, C] and [C], each or NULL (ones, zeros); NULL without post */
+  const float *w_pre, *b_pre;       /* [L+1, C] and [C], each or NULL */
+  const void *gate;                 /* [N, C], before the sigmoid; or NULL (no gate) */
+} gtp_residual;
+
+/* Statistics of both norms, [N] and [N, L+1]: written by gtp_residual_norm (each may
+ * be NULL there), read by its gradient (post's only with post). */
+typedef struct {
+  float *mean_post, *rstd_post, *mean_pre, *rstd_pre;
+} gtp_residual_stats;
+
+/* x, a, r, h: [N, C, (L+1)^2] of p->dtype; r may be x itself, else no output may
+ * overlap an input or another.  stats may be NULL.  N C == 0 is a no-op. */
+gtp_status gtp_residual_norm(const gtp_residual *p, const void *x, const void *a, void *r, void *h,
+                             const gtp_residual_stats *stats, void *stream);
+
+/* Gradients asked for, each or NULL. */
+typedef struct {
+  void *dx, *da;                    /* like x */
+  void *dgate;                      /* [N, C] of p->dtype; with a gate only */
+  float *dscale;                    /* [L+1, C] */
+  float *dw_post, *db_post;         /* [L+1, C], [C]; with post only */
+  float *dw_pre, *db_pre;           /* [L+1, C], [C] */
+} gtp_residual_grads;
+
+/* Bytes of `work` of gtp_residual_norm_backward (-1 on a bad argument). */
+int64_t gtp_residual_norm_backward_work(const gtp_residual *p);
+
+/* Gradient of gtp_residual_norm for dh and dr (like x; dr NULL: zeros), from r as it was
+ * written, a and the statistics: dx = dr + the gradient of the norm of r; with u = dx
+ * sigmoid(gate):
+ *   dscale[l, c] = sum_{n,m} u t,  dgate[n, c] = sigmoid' sum_{l,m} dx scale t,
+ *   dw_post, db_post, da: those of norm(a) w_post + b_post for u scale (post = 0: da = u scale).
+ * dx may be dr itself, else no output may overlap an input or another.  Gradients are
+ * written, not accumulated; N C == 0 writes zero weight gradients. */
+gtp_status gtp_residual_norm_backward(const gtp_residual *p, const void *r, const void *a,
+                                      const gtp_residual_stats *stats, const void *dh, const void *dr,
+                                      const gtp_residual_grads *grads, void *work, int64_t work_bytes, void *stream);
 
 /* Dropout of groups of K consecutive elements (all (L+1)^2 coefficients of a
  * channel, or K = 1) added to a residual:

@@ -140,6 +140,135 @@ gtp_status gtp_layer_norm_backward(int L, const void* x, gtp_dtype dtype, const 
   return launched(gtp::launch_norm_backward(a, static_cast<hipStream_t>(stream)), "gtp_layer_norm_backward");
 }
 
+namespace {
+
+gtp_status residual_args(const gtp_residual* p, gtp::ResArgs* g, int64_t* elems) {
+  if (!p) return bad("NULL description of the residual step");
+  const gtp_status s = norm_sizes(p->L, p->dtype, p->N, p->C, elems);
+  if (s != GTP_OK) return s;
+  if (p->post != 0 && p->post != 1) return bad("post must be 0 or 1");
+  if (!(p->eps > 0.0f) || !std::isfinite(p->eps)) return bad("eps must be positive and finite");
+  if (!p->post && (p->w_post || p->b_post)) return bad("w_post and b_post need post");
+  if (!aligned(p->scale, 4) || !aligned(p->w_post, 4) || !aligned(p->b_post, 4) || !aligned(p->w_pre, 4) ||
+      !aligned(p->b_pre, 4) || !aligned(p->gate, elem_size(p->dtype)))
+    return bad("misaligned pointer");
+  g->gate = p->gate;
+  g->scale = p->scale;
+  g->w1 = p->w_post;
+  g->b1 = p->b_post;
+  g->w2 = p->w_pre;
+  g->b2 = p->b_pre;
+  g->N = p->N;
+  g->C = p->C;
+  g->L = p->L;
+  g->bf16 = p->dtype == GTP_BF16;
+  g->post = p->post != 0;
+  g->eps = p->eps;
+  return GTP_OK;
+}
+
+// No output may overlap an input or another output, but out[same_out] may be in[same_in].
+gtp_status apart(const Span* in, int n_in, const Span* out, int n_out, int same_in, int same_out) {
+  for (int i = 0; i < n_out; ++i) {
+    for (int j = 0; j < n_in; ++j)
+      if (overlap(out[i], in[j]) && !(i == same_out && j == same_in && out[i].p == in[j].p))
+        return bad("an output overlaps an input");
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i], out[j])) return bad("two outputs overlap");
+  }
+  return GTP_OK;
+}
+
+}  // namespace
+
+gtp_status gtp_residual_norm(const gtp_residual* p, const void* x, const void* a, void* r, void* h,
+                             const gtp_residual_stats* stats, void* stream) {
+  gtp::ResArgs g{};
+  int64_t n = 0;
+  gtp_status s = residual_args(p, &g, &n);
+  if (s != GTP_OK) return s;
+  if (n == 0) return GTP_OK;
+  if (!x || !a || !r || !h) return bad("NULL data pointer");
+  const gtp_residual_stats t = stats ? *stats : gtp_residual_stats{};
+  if (!p->post && (t.mean_post || t.rstd_post)) return bad("mean_post and rstd_post need post");
+  const int64_t es = elem_size(p->dtype), w = (p->L + 1) * p->C * 4, b = p->C * 4, m = p->N * 4, d = m * (p->L + 1);
+  if (!aligned(x, es) || !aligned(a, es) || !aligned(r, es) || !aligned(h, es) || !aligned(t.mean_post, 4) ||
+      !aligned(t.rstd_post, 4) || !aligned(t.mean_pre, 4) || !aligned(t.rstd_pre, 4))
+    return bad("misaligned pointer");
+  const Span in[] = {{x, n * es}, {a, n * es}, {p->gate, p->N * p->C * es}, {p->scale, w}, {p->w_post, w},
+                     {p->b_post, b}, {p->w_pre, w}, {p->b_pre, b}};
+  const Span out[] = {{r, n * es}, {h, n * es}, {t.mean_post, m}, {t.rstd_post, d}, {t.mean_pre, m}, {t.rstd_pre, d}};
+  s = apart(in, 8, out, 6, 0, 0);
+  if (s != GTP_OK) return s;
+  g.x = x;
+  g.a = a;
+  g.r = r;
+  g.h = h;
+  g.mean1 = t.mean_post;
+  g.rstd1 = t.rstd_post;
+  g.mean2 = t.mean_pre;
+  g.rstd2 = t.rstd_pre;
+  return launched(gtp::launch_residual(g, static_cast<hipStream_t>(stream)), "gtp_residual_norm");
+}
+
+int64_t gtp_residual_norm_backward_work(const gtp_residual* p) {
+  gtp::ResArgs g{};
+  int64_t n = 0;
+  if (residual_args(p, &g, &n) != GTP_OK) return -1;
+  return n == 0 ? 0 : gtp::residual_work_floats(g) * 4;
+}
+
+gtp_status gtp_residual_norm_backward(const gtp_residual* p, const void* r, const void* a,
+                                      const gtp_residual_stats* stats, const void* dh, const void* dr,
+                                      const gtp_residual_grads* grads, void* work, int64_t work_bytes, void* stream) {
+  gtp::ResArgs g{};
+  int64_t n = 0;
+  gtp_status s = residual_args(p, &g, &n);
+  if (s != GTP_OK) return s;
+  if (!grads) return bad("NULL gradients");
+  const gtp_residual_grads& o = *grads;
+  if (!p->post && (o.dw_post || o.db_post)) return bad("dw_post and db_post need post");
+  if (!p->gate && o.dgate && n > 0) return bad("dgate needs a gate");
+  g.dx = o.dx;
+  g.da = o.da;
+  g.dgate = o.dgate;
+  g.dscale = o.dscale;
+  g.dw1 = o.dw_post;
+  g.db1 = o.db_post;
+  g.dw2 = o.dw_pre;
+  g.db2 = o.db_pre;
+  if (p->C == 0 || !(g.dx || g.da || g.dgate || g.weights())) return GTP_OK;
+  const gtp_residual_stats t = stats ? *stats : gtp_residual_stats{};
+  if (n > 0 && (!r || !a || !dh || !t.mean_pre || !t.rstd_pre || (p->post && (!t.mean_post || !t.rstd_post))))
+    return bad("NULL data pointer");
+  const int64_t es = elem_size(p->dtype), w = (p->L + 1) * p->C * 4, b = p->C * 4, m = p->N * 4, d = m * (p->L + 1);
+  if (!aligned(r, es) || !aligned(a, es) || !aligned(dh, es) || !aligned(dr, es) || !aligned(o.dx, es) ||
+      !aligned(o.da, es) || !aligned(o.dgate, es) || !aligned(t.mean_post, 4) || !aligned(t.rstd_post, 4) ||
+      !aligned(t.mean_pre, 4) || !aligned(t.rstd_pre, 4) || !aligned(o.dscale, 4) || !aligned(o.dw_post, 4) ||
+      !aligned(o.db_post, 4) || !aligned(o.dw_pre, 4) || !aligned(o.db_pre, 4) || !aligned(work, 16))
+    return bad("misaligned pointer");
+  const int64_t need = n > 0 ? gtp::residual_work_floats(g) * 4 : 0;
+  if (need > 0 && (!work || work_bytes < need))
+    return bad("work is smaller than gtp_residual_norm_backward_work says");
+  const Span in[] = {{dr, n * es}, {r, n * es}, {a, n * es}, {dh, n * es}, {p->gate, p->N * p->C * es}, {p->scale, w},
+                     {p->w_post, w}, {p->b_post, b}, {p->w_pre, w}, {p->b_pre, b}, {p->post ? t.mean_post : nullptr, m},
+                     {p->post ? t.rstd_post : nullptr, d}, {t.mean_pre, m}, {t.rstd_pre, d}};
+  const Span out[] = {{o.dx, n * es}, {o.da, n * es}, {o.dgate, p->N * p->C * es}, {o.dscale, w}, {o.dw_post, w},
+                      {o.db_post, b}, {o.dw_pre, w}, {o.db_pre, b}, {need > 0 ? work : nullptr, need}};
+  s = apart(in, 14, out, 9, 0, 0);
+  if (s != GTP_OK) return s;
+  g.x = r;
+  g.a = a;
+  g.dh = dh;
+  g.dr = dr;
+  g.mean1 = t.mean_post;
+  g.rstd1 = t.rstd_post;
+  g.mean2 = t.mean_pre;
+  g.rstd2 = t.rstd_pre;
+  g.work = static_cast<float*>(work);
+  return launched(gtp::launch_residual_backward(g, static_cast<hipStream_t>(stream)), "gtp_residual_norm_backward");
+}
+
 gtp_status gtp_dropout(const void* x, const void* res, gtp_dtype dtype, double p, const uint64_t* rng, int64_t groups,
                        int64_t K, void* y, void* stream) {
   if (!dtype_known(dtype)) return bad("dtype must be GTP_F32 or GTP_BF16");

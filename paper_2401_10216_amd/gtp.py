@@ -60,6 +60,9 @@ class _Attn(ctypes.Structure):
 _ATTN = struct.Struct("<4i5q3Qf4xdQ")
 _ROWS = "Qqq"
 assert _ATTN.size == ctypes.sizeof(_Attn) and struct.calcsize("<" + _ROWS) == ctypes.sizeof(_Rows)
+_RESIDUAL = struct.Struct("<2i2qif6Q")  # gtp_residual
+_RESIDUAL_STATS = struct.Struct("<4Q")  # gtp_residual_stats
+_RESIDUAL_GRADS = struct.Struct("<8Q")  # gtp_residual_grads
 
 _SIGS = {
     "gtp_plan_create": (_I, [ctypes.POINTER(_P), _I, _I, _I, _U]),
@@ -79,6 +82,9 @@ _SIGS = {
     "gtp_layer_norm": (_I, [_I, _P, _I, _P, _P, ctypes.c_float, _I64, _I64, _P, _P, _P, _P]),
     "gtp_layer_norm_backward_work": (_I64, [_I, _I, _I64, _I64]),
     "gtp_layer_norm_backward": (_I, [_I, _P, _I, _P, _P, _P, _P, _I64, _I64, _P, _P, _P, _P, _I64, _P]),
+    "gtp_residual_norm": (_I, [_P, _P, _P, _P, _P, _P, _P]),
+    "gtp_residual_norm_backward_work": (_I64, [_P]),
+    "gtp_residual_norm_backward": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _I64, _P]),
     "gtp_dropout": (_I, [_P, _P, _I, ctypes.c_double, _P, _I64, _I64, _P, _P]),
     "gtp_attention_work": (_I64, [_P, _I]),
     "gtp_attention": (_I, [_P, _P, _P, _P, _P, _P, _P, _I64, _P]),
@@ -579,6 +585,94 @@ def gtp_layer_norm_backward(x, dy, L: int, mean, rstd, w=None, need=("dx", "dw",
         work = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes > 0 else None
     _check(lib_.gtp_layer_norm_backward(L, px, code, pw, pm, pr, pdy, N, C, _ptr(out.get("dx")), _ptr(out.get("dw")),
                                         _ptr(out.get("db")), _ptr(work), nbytes, _stream(stream)), lib_)
+    return out
+
+
+def _residual(x, a, L, gate, scale, w_post, b_post, w_pre, b_pre, post, eps):
+    """Validated fields of gtp_residual, and the data pointers of x and a."""
+    if x.dim() != 3 or x.shape[2] != nsh(L):
+        raise ValueError("x must be [N, C, (L+1)^2]")
+    N, C, _ = x.shape
+    dev, one, own = x.device, _f32(), (x.dtype,)
+    code = _dtype_code(x)
+    if not post and (w_post is not None or b_post is not None):
+        raise ValueError("w_post and b_post need post")
+    ptr = [_opt(t, name, shape, types, dev) or 0 for t, name, shape, types in (
+        (scale, "scale", (L + 1, C), one), (w_post, "w_post", (L + 1, C), one), (b_post, "b_post", (C,), one),
+        (w_pre, "w_pre", (L + 1, C), one), (b_pre, "b_pre", (C,), one), (gate, "gate", (N, C), own))]
+    return (L, code, N, C, 1 if post else 0, eps, *ptr), _want(x, "x", x.shape, own), _want(a, "a", x.shape, own, dev)
+
+
+def gtp_residual_norm(x, a, L: int, gate=None, scale=None, w_post=None, b_post=None, w_pre=None, b_pre=None,
+                      post: bool = True, eps: float = 1e-5, r=None, h=None, stream=None):
+    """(r, h, stats): the residual step r = x + scale sigmoid(gate) t between two parts of a block and its norm
+    h = norm(r) w_pre + b_pre, for a part's output a[N, C, (L+1)^2] and the residual stream x (like a), with
+    t = norm(a) w_post + b_post (post=False: t = a); norms as in gtp_layer_norm, shifts at degree 0.  scale, w_post,
+    w_pre: [L+1, C] fp32, b_post, b_pre: [C] fp32, gate: [N, C] of x's type, each or None (ones, zeros, no gate).
+    stats = (mean_post, rstd_post, mean_pre, rstd_pre), fp32 [N] and [N, L+1] (post's None without post), is what the
+    backward reads.  r may be x."""
+    import torch
+    f32 = torch.float32
+    desc, px, pa = _residual(x, a, L, gate, scale, w_post, b_post, w_pre, b_pre, post, eps)
+    N, dev, own = x.shape[0], x.device, (x.dtype,)
+    with _allocating(stream):
+        r = torch.empty_like(x) if r is None else r
+        h = torch.empty_like(x) if h is None else h
+        stats = tuple(torch.empty(shape, dtype=f32, device=dev) if post or i > 1 else None
+                      for i, shape in enumerate(((N,), (N, L + 1)) * 2))
+    pr = _want(r, "r", x.shape, own, dev)
+    ph = _want(h, "h", x.shape, own, dev)
+    _on_gpu(x, "x")
+    lib_ = lib()
+    _check(lib_.gtp_residual_norm(_RESIDUAL.pack(*desc), px, pa, pr, ph,
+                                  _RESIDUAL_STATS.pack(*[_ptr(t) or 0 for t in stats]), _stream(stream)), lib_)
+    return r, h, stats
+
+
+_RESIDUAL_NEED = ("dx", "da", "dgate", "dscale", "dw_post", "db_post", "dw_pre", "db_pre")
+
+
+def gtp_residual_norm_backward(r, a, L: int, stats, dh, dr=None, gate=None, scale=None, w_post=None, b_post=None,
+                               w_pre=None, b_pre=None, post: bool = True, need=None, dx=None, stream=None):
+    """Gradients of <dh, h> + <dr, r> of gtp_residual_norm, whose results r and stats and other arguments it takes
+    (dr None: zeros): a dict with the keys of need (None: all there are) among dx, da (like r), dgate[N, C] (with a
+    gate), dscale[L+1, C], dw_post[L+1, C], db_post[C] (with post), dw_pre[L+1, C], db_pre[C] (fp32).  dx: a tensor to
+    write to, which may be dr."""
+    import torch
+    f32 = torch.float32
+    desc, pr, pa = _residual(r, a, L, gate, scale, w_post, b_post, w_pre, b_pre, post, 1.0)
+    N, C, _ = r.shape
+    dev, own, one = r.device, (r.dtype,), _f32()
+    there = [n for n in _RESIDUAL_NEED if (gate is not None or n != "dgate") and (post or not n.endswith("_post"))]
+    need = there if need is None else need
+    unknown = set(need) - set(there)
+    if unknown:
+        raise ValueError(f"unknown gradients {sorted(unknown)}")
+    if len(stats) != 4:
+        raise ValueError("stats must be what gtp_residual_norm returned")
+    ps = [_want(t, name, shape, one, dev) if post or i > 1 else 0 for i, (t, name, shape) in enumerate(zip(
+        stats, ("mean_post", "rstd_post", "mean_pre", "rstd_pre"), ((N,), (N, L + 1)) * 2))]
+    pdh = _want(dh, "dh", r.shape, own, dev)
+    pdr = _opt(dr, "dr", r.shape, own, dev)
+    _on_gpu(r, "r")
+    lib_ = lib()
+    d = _RESIDUAL.pack(*desc)
+    nbytes = lib_.gtp_residual_norm_backward_work(d)
+    out = {}
+    with _allocating(stream):
+        for n in need:
+            if n in ("dx", "da"):
+                out[n] = dx if n == "dx" and dx is not None else torch.empty_like(r)
+            elif n == "dgate":
+                out[n] = torch.empty((N, C), dtype=r.dtype, device=dev)
+            else:
+                out[n] = torch.empty((C,) if n.startswith("db") else (L + 1, C), dtype=f32, device=dev)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes > 0 else None
+    if dx is not None and "dx" in out:
+        _want(dx, "dx", r.shape, own, dev)
+    _check(lib_.gtp_residual_norm_backward(d, pr, pa, _RESIDUAL_STATS.pack(*ps), pdh, pdr,
+                                           _RESIDUAL_GRADS.pack(*[_ptr(out.get(n)) or 0 for n in _RESIDUAL_NEED]),
+                                           _ptr(work), nbytes, _stream(stream)), lib_)
     return out
 
 
