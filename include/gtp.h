@@ -467,6 +467,42 @@ gtp_status gtp_attention_backward(const gtp_attn *a, const gtp_rows *q, const gt
                                   const gtp_rows *o, const gtp_rows *dout, const float *lse, const gtp_rows *dq,
                                   const gtp_rows *dk, const gtp_rows *dv, void *work, int64_t work_bytes, void *stream);
 
+/* A learned bias of the scores by the distance of the atoms, for each query head and
+ * bucket of the squared distance d2 of a query's and a key's position:
+ *   bucket 0 where d2 < r0sq,  else 1 + (number(d2) - number(r0sq)) >> shift,  at most buckets - 1,
+ * number(x) the place of a positive fp32 number among them (its bits as an integer), so
+ * that each doubling of d2 has per_octave = 2^(23 - shift) buckets, evenly spaced between
+ * powers of two; the last bucket is open.  d2 = dx^2 + dy^2 + dz^2 in fp32 with one rounding for
+ * each difference, for dx^2 and for each of the two sums (fma), so a pair has the same bucket
+ * everywhere.  A pair whose d2 is NaN is in the last bucket.  -infinity in the bias gives a
+ * bucket's pairs probability zero (a cutoff).  Positions of absent keys may hold anything. */
+typedef struct {
+  const float *bias;                /* [H, buckets] */
+  const float *q_pos, *k_pos;       /* [Tq, 3], [Tk, 3] */
+  float r0sq;                       /* 2^-100 at least; the last bucket's edge must be finite */
+  int buckets;                      /* 1..64 */
+  int per_octave;                   /* 1, 2, 4, 8 or 16 */
+} gtp_attn_bias;
+
+/* The first squared distances of buckets 1 .. buckets - 1 (host memory, buckets - 1 floats). */
+gtp_status gtp_attention_bias_edges(float r0sq, int buckets, int per_octave, float *edges);
+
+/* gtp_attention with a bias: s = scale q k^T + bias[h, bucket] (b: not NULL; the bias's values are
+ * multiplied by log2(e), within fp32's range).  GTP_ERR_UNSUPPORTED where the query heads of a key head
+ * have more than 4096 biases in all.  Else as gtp_attention. */
+int64_t gtp_attention_biased_work(const gtp_attn *a, const gtp_attn_bias *b, int backward);
+gtp_status gtp_attention_biased(const gtp_attn *a, const gtp_attn_bias *b, const gtp_rows *q, const gtp_rows *k,
+                                const gtp_rows *v, const gtp_rows *o, float *lse, void *work, int64_t work_bytes,
+                                void *stream);
+
+/* Its gradient: dq, dk, dv as gtp_attention_backward, and
+ *   dbias[h, c] = sum of dS over the pairs of bucket c   [H, buckets] fp32, or NULL,
+ * written, not accumulated, summed in a fixed order.  Positions have no gradient: the bias is piecewise constant. */
+gtp_status gtp_attention_biased_backward(const gtp_attn *a, const gtp_attn_bias *b, const gtp_rows *q,
+                                         const gtp_rows *k, const gtp_rows *v, const gtp_rows *o, const gtp_rows *dout,
+                                         const float *lse, const gtp_rows *dq, const gtp_rows *dk, const gtp_rows *dv,
+                                         float *dbias, void *work, int64_t work_bytes, void *stream);
+
 /* HBM streaming probe (measurement aid: the roof the HBM-bound kernels are
  * read against; each workgroup streams one contiguous chunk, the chunks
  * dealt to the XCDs in contiguous runs).  mode 0: read nbytes of src (dst: a

@@ -26,8 +26,13 @@ struct AttnArgs {
   float* part;                   // results of the parts of a split call, [splits, rows, d] (forward: then [splits, rows]
                                  // of lse; dk, dv: one behind the other)
   const uint64_t* rng;           // {seed, offset}, with threshold > 0
+  const float *bias, *q_pos, *k_pos;  // [H, buckets] added to the scores by distance; positions [Tq, 3], [Tk, 3]; or null
+  float* dbias;                  // [H, buckets]: gradient asked for, or null
+  float* bias_part;              // bias_part_floats, for dbias
   int64_t B, Tq, Tk, max_q, max_k;
   int H, Hk, G, d;               // query heads, key heads, H / Hk, head length
+  int buckets;                   // of the bias
+  uint32_t near, far, step;      // bucket of a squared distance: see Buckets
   int splits;                    // parts that a row's keys (or a key's rows) are dealt to
   float scale, scale2;           // of the scores; times log2(e)
   uint32_t threshold;            // 0: nothing is dropped
@@ -38,12 +43,23 @@ struct AttnArgs {
 // Rows (keys in dk, dv) that a workgroup takes, a wave 32: 128, or 64 where no segment has
 // more, so that short ones do not leave half the waves idle.
 inline int rows_a_tile(int64_t most) { return most <= 64 ? 64 : 128; }
+constexpr int kMaxBias = 4096;  // floats of the bias of a key head's query heads, in LDS
+int dq_rows_a_tile(const AttnArgs& a);  // of dq: a bias's sums beside the longest fp32 tiles fit the LDS of 64 rows only
 int attn_padded(int d);  // the head length that the kernels are instantiated at, >= d
 // Parts that the keys of each row (the rows of each key) are dealt to: 1 where the
 // workgroups fill the chip without.
 int attn_row_splits(const AttnArgs& a, bool backward);  // its parts: of the forward, of dq
 int attn_key_splits(const AttnArgs& a);
 hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t s);
+// With a bias (instantiations of their own, gtp_attn_bias_*.hip).
+void launch_attn_fwd_bias(const AttnArgs& a, hipStream_t s);
+void launch_attn_dq_bias(const AttnArgs& a, hipStream_t s);
+void launch_attn_dkv_bias(const AttnArgs& a, hipStream_t s);
+// Workgroups of dq with a bias that work on one key head, floats for what each leaves of
+// dbias and for their sums, and the sum of them all (a.splits: of dq).
+int64_t attn_bias_parts(const AttnArgs& a);
+int64_t bias_part_floats(const AttnArgs& a);
+hipError_t launch_attn_bias_sum(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_delta(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_dq(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_dkv(const AttnArgs& a, hipStream_t s);

@@ -561,6 +561,51 @@ struct Drop {
   }
 };
 
+// The learned bias of a score, by the distance of its two positions: bucket
+//   0 where d2 < r0^2,  1 + (number(d2) - number(r0^2)) >> shift,  at most buckets - 1,
+// number(x) the place of a positive fp32 number among them all, its bits: 2^(23 - shift)
+// buckets for each doubling of d2, evenly spaced between powers of two.  d2 = dx^2 + dy^2 + dz^2
+// with one rounding for each difference, for dx^2 and for each sum, so that every pass, and
+// whoever computes it elsewhere, finds the same bucket.  NaN is above every number, whatever its sign bit.
+// Three instructions from d2 to the bucket; an exact logarithm, or a search among edges in
+// LDS, would be several times that beside the 10-20 that a score takes in all.
+struct Buckets {
+  uint32_t near, far, shift;  // numbers of the first bucket's and the last's first d2 (near: a step below r0^2)
+  __device__ __forceinline__ explicit Buckets(const AttnArgs& a) : near(a.near), far(a.far), shift(a.step) {}
+  __device__ __forceinline__ uint32_t operator()(float dx, float dy, float dz) const {
+    const float d2 = fmaf(dz, dz, fmaf(dy, dy, __fmul_rn(dx, dx)));
+    uint32_t v = __float_as_uint(d2);
+    v = v < near ? near : v;
+    v = v > far ? far : v;
+    return (v - near) >> shift;
+  }
+};
+
+// The bias of key head hk's query heads in LDS, in units of log 2: [G][buckets].
+__device__ __forceinline__ void load_bias(const AttnArgs& a, int hk, float* table) {
+  const int n = a.G * a.buckets;
+  const float* const from = a.bias + int64_t(hk) * n;
+  for (int i = threadIdx.x; i < n; i += int(blockDim.x)) table[i] = from[i] * kLog2e;
+}
+
+// Positions of a tile's rows, one after the other x, y, z [ROWS] each in LDS: a lane fetches row lane % ROWS's.
+template <int ROWS>
+struct StagedPos {
+  float x, y, z;
+  __device__ __forceinline__ void fetch(const float* pos, int64_t row) {
+    x = pos[3 * row];
+    y = pos[3 * row + 1];
+    z = pos[3 * row + 2];
+  }
+  __device__ __forceinline__ void commit(float* tile) const {
+    if (threadIdx.x < ROWS) {
+      tile[threadIdx.x] = x;
+      tile[ROWS + threadIdx.x] = y;
+      tile[2 * ROWS + threadIdx.x] = z;
+    }
+  }
+};
+
 // Waves a SIMD that a kernel's registers are cut for: two hide each other's
 // waits (one issues vector instructions while the matrix unit works for the
 // other), where rows, accumulators and a prefetched tile of a four-wave workgroup fit

@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
+#include <cstring>
 
 #include "gtp_attn.hpp"
 #include "gtp_rng.hpp"
@@ -411,19 +412,69 @@ gtp_status attn_sizes(const gtp_attn* a, gtp::AttnArgs* g) {
 gtp::AttnRows rows_of(const gtp_rows* r) { return r ? gtp::AttnRows{r->data, r->row, r->head} : gtp::AttnRows{}; }
 
 // The forward: the parts of a split call and their lse.  The backward: the rows'
-// deltas, then the parts of dq or of dk and dv, one after the other in the same place.
+// deltas, what the workgroups leave of a bias's gradient, then the parts of dq or of dk
+// and dv, one after the other in the same place.
 int64_t delta_bytes(const gtp::AttnArgs& g) { return (g.Tq * g.H * 4 + 15) / 16 * 16; }
+int64_t bias_bytes(gtp::AttnArgs g) {
+  if (!g.bias) return 0;
+  g.splits = gtp::attn_row_splits(g, true);
+  return (gtp::bias_part_floats(g) * 4 + 15) / 16 * 16;
+}
 int64_t attn_work(const gtp::AttnArgs& g, int backward) {
   const int64_t s = gtp::attn_row_splits(g, backward), rows = s > 1 ? s * g.Tq * g.H * (g.d + (backward ? 0 : 1)) * 4 : 0;
   if (!backward) return rows;
   const int64_t t = gtp::attn_key_splits(g), keys = t > 1 ? 2 * t * g.Tk * g.Hk * g.d * 4 : 0;
-  return delta_bytes(g) + (rows > keys ? rows : keys);
+  return delta_bytes(g) + bias_bytes(g) + (rows > keys ? rows : keys);
+}
+
+constexpr float kNearest = 0x1p-100f;
+
+// near, far and shift of Buckets; false where the last edge is not finite.
+bool bucket_numbers(float r0sq, int buckets, int per_octave, uint32_t* near, uint32_t* far, uint32_t* shift) {
+  uint32_t first = 0;
+  std::memcpy(&first, &r0sq, 4);
+  int octave = 0;
+  while ((1 << octave) < per_octave) ++octave;
+  *shift = uint32_t(23 - octave);
+  *near = first - (1u << *shift);
+  const uint64_t last = buckets < 2 ? *near : first + (uint64_t(buckets - 2) << *shift);
+  *far = uint32_t(last);
+  return last < 0x7f800000u;
+}
+
+const char* bias_numbers_why(float r0sq, int buckets, int per_octave) {
+  if (!(r0sq >= kNearest) || !std::isfinite(r0sq)) return "r0sq must be 2^-100 at least and finite";
+  if (buckets < 1 || buckets > 64) return "buckets must be in 1..64";
+  if (per_octave < 1 || per_octave > 16 || (per_octave & (per_octave - 1)) != 0)
+    return "per_octave must be 1, 2, 4, 8 or 16";
+  uint32_t near, far, shift;
+  if (!bucket_numbers(r0sq, buckets, per_octave, &near, &far, &shift)) return "the last bucket's edge must be finite";
+  return nullptr;
+}
+
+gtp_status bias_args(const gtp_attn_bias* b, gtp::AttnArgs* g) {
+  if (!b) return bad("NULL description of the bias");
+  if (const char* why = bias_numbers_why(b->r0sq, b->buckets, b->per_octave)) return bad(why);
+  if (int64_t(g->G) * b->buckets > gtp::kMaxBias) return unsupported("more than 4096 biases for a key head's query heads");
+  if (!b->bias || (!b->q_pos && g->Tq > 0) || (!b->k_pos && g->Tk > 0)) return bad("NULL data pointer");
+  if (!aligned(b->bias, 4) || !aligned(b->q_pos, 4) || !aligned(b->k_pos, 4)) return bad("misaligned pointer");
+  g->bias = b->bias;
+  g->q_pos = b->q_pos;
+  g->k_pos = b->k_pos;
+  g->buckets = b->buckets;
+  bucket_numbers(b->r0sq, b->buckets, b->per_octave, &g->near, &g->far, &g->step);
+  // what dq's workgroups leave of the bias's gradient, counted generously
+  int64_t n = 0;
+  if (!times((g->max_q * g->G + 63) / 64 * 128, g->B, &n) || !times(n, int64_t(g->H) * g->buckets, &n) ||
+      n > kMaxElems >> 10)
+    return unsupported("more workgroups than the work's size can count");
+  return GTP_OK;
 }
 
 // Checks of `n` inputs and outputs against each other, the row statistics, the
 // work and the index arrays.
 gtp_status attn_memory(const gtp_attn* a, const Rows* in, int n_in, const Rows* out, int n_out, Span lse, bool lse_out,
-                       Span work, bool* vec) {
+                       Span work, bool* vec, const gtp_attn_bias* b, Span dbias) {
   const int64_t es = elem_size(a->dtype);
   const char* why = nullptr;
   *vec = a->d * es % 16 == 0;
@@ -438,8 +489,10 @@ gtp_status attn_memory(const gtp_attn* a, const Rows* in, int n_in, const Rows* 
   }
   if (lse.bytes > 0 && !lse.p) return bad("NULL data pointer");
   if (!aligned(lse.p, 4) || !aligned(work.p, 16)) return bad("misaligned pointer");
-  const Span small[] = {{a->q_off, (a->B + 1) * 8}, {a->k_off, (a->B + 1) * 8}, {a->key_mask, a->Tk}, {a->rng, 16}};
-  const Span own[] = {lse, work};
+  const Span small[] = {{a->q_off, (a->B + 1) * 8}, {a->k_off, (a->B + 1) * 8}, {a->key_mask, a->Tk}, {a->rng, 16},
+                        {b ? b->bias : nullptr, b ? int64_t(a->H) * b->buckets * 4 : 0},
+                        {b ? b->q_pos : nullptr, a->Tq * 12}, {b ? b->k_pos : nullptr, a->Tk * 12}};
+  const Span own[] = {lse, work, dbias};
   for (int i = 0; i < n_out; ++i) {
     if (!out[i].r || out[i].T == 0) continue;
     const Span o{out[i].r->data, extent(out[i], a->d, es)};
@@ -450,16 +503,94 @@ gtp_status attn_memory(const gtp_attn* a, const Rows* in, int n_in, const Rows* 
     for (const Span& t : small)
       if (overlap(o, t)) return bad("an output overlaps an input");
     for (const Span& t : own)
-      if (overlap(o, t)) return bad("an output overlaps lse or work");
+      if (overlap(o, t)) return bad("an output overlaps lse, work or dbias");
   }
   for (int j = 0; j < n_in; ++j) {
     if (!in[j].r || in[j].T == 0) continue;
     const Span i{in[j].r->data, extent(in[j], a->d, es)};
-    if (overlap(work, i) || (lse_out && overlap(lse, i))) return bad("lse or work overlaps an input");
+    if (overlap(work, i) || overlap(dbias, i) || (lse_out && overlap(lse, i)))
+      return bad("lse, work or dbias overlaps an input");
   }
   for (const Span& t : small)
-    if (overlap(work, t) || (lse_out && overlap(lse, t))) return bad("lse or work overlaps an input");
+    if (overlap(work, t) || overlap(dbias, t) || (lse_out && overlap(lse, t)))
+      return bad("lse, work or dbias overlaps an input");
+  if (overlap(dbias, lse) || overlap(dbias, work)) return bad("dbias overlaps lse or work");
   return overlap(lse, work) ? bad("lse overlaps work") : GTP_OK;
+}
+
+gtp_status attention(const gtp_attn* a, const gtp_attn_bias* b, bool biased, const gtp_rows* q, const gtp_rows* k,
+                     const gtp_rows* v, const gtp_rows* o, float* lse, void* work, int64_t work_bytes, void* stream,
+                     const char* name) {
+  gtp::AttnArgs g{};
+  gtp_status s = attn_sizes(a, &g);
+  if (s == GTP_OK && biased) s = bias_args(b, &g);
+  if (s != GTP_OK) return s;
+  const int64_t need = attn_work(g, 0);
+  if (need > 0 && (!work || work_bytes < need)) return bad("work is smaller than its size function says");
+  if (a->Tq > 0 && !o) return bad("NULL data pointer");
+  const Rows in[] = {{q, a->Tq, a->H}, {k, a->Tk, a->Hk}, {v, a->Tk, a->Hk}}, out[] = {{o, a->Tq, a->H}};
+  s = attn_memory(a, in, 3, out, 1, {lse, a->Tq * a->H * 4}, true, {need > 0 ? work : nullptr, need}, &g.vec, b, {});
+  if (s != GTP_OK) return s;
+  if (a->B == 0 || a->max_q == 0) return GTP_OK;
+  g.q = rows_of(q);
+  g.k = rows_of(k);
+  g.v = rows_of(v);
+  g.out = rows_of(o);
+  g.lse = lse;
+  g.part = static_cast<float*>(work);
+  g.splits = gtp::attn_row_splits(g, false);
+  return launched(gtp::launch_attn_fwd(g, static_cast<hipStream_t>(stream)), name);
+}
+
+gtp_status attention_backward(const gtp_attn* a, const gtp_attn_bias* b, bool biased, const gtp_rows* q,
+                              const gtp_rows* k, const gtp_rows* v, const gtp_rows* o, const gtp_rows* dout,
+                              const float* lse, const gtp_rows* dq, const gtp_rows* dk, const gtp_rows* dv,
+                              float* dbias, void* work, int64_t work_bytes, void* stream, const char* name) {
+  gtp::AttnArgs g{};
+  gtp_status s = attn_sizes(a, &g);
+  if (s == GTP_OK && biased) s = bias_args(b, &g);
+  if (s != GTP_OK) return s;
+  if ((dk == nullptr) != (dv == nullptr)) return bad("dk and dv are computed together");
+  if (!dq && !dk && !dbias) return GTP_OK;
+  if (!aligned(dbias, 4)) return bad("misaligned pointer");
+  const int64_t need = attn_work(g, 1);
+  if (need > 0 && (!work || work_bytes < need)) return bad("work is smaller than its size function says");
+  const Rows in[] = {{q, a->Tq, a->H}, {k, a->Tk, a->Hk}, {v, a->Tk, a->Hk}, {o, a->Tq, a->H}, {dout, a->Tq, a->H}};
+  const Rows out[] = {{dq, a->Tq, a->H}, {dk, a->Tk, a->Hk}, {dv, a->Tk, a->Hk}};
+  s = attn_memory(a, in, 5, out, 3, {lse, a->Tq * a->H * 4}, false, {need > 0 ? work : nullptr, need}, &g.vec, b,
+                  {dbias, dbias ? int64_t(a->H) * b->buckets * 4 : 0});
+  if (s != GTP_OK) return s;
+  if (a->B == 0 && !dbias) return GTP_OK;
+  g.q = rows_of(q);
+  g.k = rows_of(k);
+  g.v = rows_of(v);
+  g.o = rows_of(o);
+  g.dout = rows_of(dout);
+  g.out = rows_of(dq);
+  g.dk = rows_of(dk);
+  g.dv = rows_of(dv);
+  g.lse = const_cast<float*>(lse);
+  g.dbias = dbias;
+  g.delta = static_cast<float*>(work);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  hipError_t e = a->B > 0 && a->Tq > 0 ? gtp::launch_attn_delta(g, st) : hipSuccess;
+  char* const past = static_cast<char*>(work) + delta_bytes(g);
+  g.bias_part = reinterpret_cast<float*>(past);
+  g.part = reinterpret_cast<float*>(past + bias_bytes(g));
+  if (e == hipSuccess && (dq || dbias) && a->B > 0 && a->max_q > 0) {
+    g.splits = gtp::attn_row_splits(g, true);
+    e = gtp::launch_attn_dq(g, st);
+    if (e == hipSuccess && dq && g.splits > 1) e = gtp::launch_attn_sum(g, g.part, g.splits, false, g.out, st);
+  }
+  if (e == hipSuccess && dbias) e = gtp::launch_attn_bias_sum(g, st);
+  if (e == hipSuccess && dk && a->B > 0 && a->max_k > 0) {
+    g.splits = gtp::attn_key_splits(g);
+    e = gtp::launch_attn_dkv(g, st);
+    const int64_t one = g.splits * g.Tk * g.Hk * g.d;
+    if (e == hipSuccess && g.splits > 1) e = gtp::launch_attn_sum(g, g.part, g.splits, true, g.dk, st);
+    if (e == hipSuccess && g.splits > 1) e = gtp::launch_attn_sum(g, g.part + one, g.splits, true, g.dv, st);
+  }
+  return launched(e, name);
 }
 
 }  // namespace
@@ -474,68 +605,47 @@ int64_t gtp_attention_work(const gtp_attn* a, int backward) {
 
 gtp_status gtp_attention(const gtp_attn* a, const gtp_rows* q, const gtp_rows* k, const gtp_rows* v, const gtp_rows* o,
                          float* lse, void* work, int64_t work_bytes, void* stream) {
-  gtp::AttnArgs g{};
-  gtp_status s = attn_sizes(a, &g);
-  if (s != GTP_OK) return s;
-  const int64_t need = attn_work(g, 0);
-  if (need > 0 && (!work || work_bytes < need)) return bad("work is smaller than gtp_attention_work says");
-  if (a->Tq > 0 && !o) return bad("NULL data pointer");
-  const Rows in[] = {{q, a->Tq, a->H}, {k, a->Tk, a->Hk}, {v, a->Tk, a->Hk}}, out[] = {{o, a->Tq, a->H}};
-  s = attn_memory(a, in, 3, out, 1, {lse, a->Tq * a->H * 4}, true, {need > 0 ? work : nullptr, need}, &g.vec);
-  if (s != GTP_OK) return s;
-  if (a->B == 0 || a->max_q == 0) return GTP_OK;
-  g.q = rows_of(q);
-  g.k = rows_of(k);
-  g.v = rows_of(v);
-  g.out = rows_of(o);
-  g.lse = lse;
-  g.part = static_cast<float*>(work);
-  g.splits = gtp::attn_row_splits(g, false);
-  return launched(gtp::launch_attn_fwd(g, static_cast<hipStream_t>(stream)), "gtp_attention");
+  return attention(a, nullptr, false, q, k, v, o, lse, work, work_bytes, stream, "gtp_attention");
 }
 
 gtp_status gtp_attention_backward(const gtp_attn* a, const gtp_rows* q, const gtp_rows* k, const gtp_rows* v,
                                   const gtp_rows* o, const gtp_rows* dout, const float* lse, const gtp_rows* dq,
                                   const gtp_rows* dk, const gtp_rows* dv, void* work, int64_t work_bytes,
                                   void* stream) {
+  return attention_backward(a, nullptr, false, q, k, v, o, dout, lse, dq, dk, dv, nullptr, work, work_bytes, stream,
+                            "gtp_attention_backward");
+}
+
+gtp_status gtp_attention_bias_edges(float r0sq, int buckets, int per_octave, float* edges) {
+  if (const char* why = bias_numbers_why(r0sq, buckets, per_octave)) return bad(why);
+  if (!edges && buckets > 1) return bad("NULL data pointer");
+  uint32_t near, far, shift;
+  bucket_numbers(r0sq, buckets, per_octave, &near, &far, &shift);
+  for (int i = 1; i < buckets; ++i) {
+    const uint32_t bits = near + (uint32_t(i) << shift);
+    std::memcpy(edges + i - 1, &bits, 4);
+  }
+  return GTP_OK;
+}
+
+int64_t gtp_attention_biased_work(const gtp_attn* a, const gtp_attn_bias* b, int backward) {
   gtp::AttnArgs g{};
-  gtp_status s = attn_sizes(a, &g);
-  if (s != GTP_OK) return s;
-  if ((dk == nullptr) != (dv == nullptr)) return bad("dk and dv are computed together");
-  if (!dq && !dk) return GTP_OK;
-  const int64_t need = attn_work(g, 1);
-  if (need > 0 && (!work || work_bytes < need)) return bad("work is smaller than gtp_attention_work says");
-  const Rows in[] = {{q, a->Tq, a->H}, {k, a->Tk, a->Hk}, {v, a->Tk, a->Hk}, {o, a->Tq, a->H}, {dout, a->Tq, a->H}};
-  const Rows out[] = {{dq, a->Tq, a->H}, {dk, a->Tk, a->Hk}, {dv, a->Tk, a->Hk}};
-  s = attn_memory(a, in, 5, out, 3, {lse, a->Tq * a->H * 4}, false, {need > 0 ? work : nullptr, need}, &g.vec);
-  if (s != GTP_OK) return s;
-  if (a->B == 0) return GTP_OK;
-  g.q = rows_of(q);
-  g.k = rows_of(k);
-  g.v = rows_of(v);
-  g.o = rows_of(o);
-  g.dout = rows_of(dout);
-  g.out = rows_of(dq);
-  g.dk = rows_of(dk);
-  g.dv = rows_of(dv);
-  g.lse = const_cast<float*>(lse);
-  g.delta = static_cast<float*>(work);
-  const hipStream_t st = static_cast<hipStream_t>(stream);
-  hipError_t e = a->Tq > 0 ? gtp::launch_attn_delta(g, st) : hipSuccess;
-  g.part = reinterpret_cast<float*>(static_cast<char*>(work) + delta_bytes(g));
-  if (e == hipSuccess && dq && a->max_q > 0) {
-    g.splits = gtp::attn_row_splits(g, true);
-    e = gtp::launch_attn_dq(g, st);
-    if (e == hipSuccess && g.splits > 1) e = gtp::launch_attn_sum(g, g.part, g.splits, false, g.out, st);
-  }
-  if (e == hipSuccess && dk && a->max_k > 0) {
-    g.splits = gtp::attn_key_splits(g);
-    e = gtp::launch_attn_dkv(g, st);
-    const int64_t one = g.splits * g.Tk * g.Hk * g.d;
-    if (e == hipSuccess && g.splits > 1) e = gtp::launch_attn_sum(g, g.part, g.splits, true, g.dk, st);
-    if (e == hipSuccess && g.splits > 1) e = gtp::launch_attn_sum(g, g.part + one, g.splits, true, g.dv, st);
-  }
-  return launched(e, "gtp_attention_backward");
+  if (attn_sizes(a, &g) != GTP_OK || bias_args(b, &g) != GTP_OK) return -1;
+  return attn_work(g, backward);
+}
+
+gtp_status gtp_attention_biased(const gtp_attn* a, const gtp_attn_bias* b, const gtp_rows* q, const gtp_rows* k,
+                                const gtp_rows* v, const gtp_rows* o, float* lse, void* work, int64_t work_bytes,
+                                void* stream) {
+  return attention(a, b, true, q, k, v, o, lse, work, work_bytes, stream, "gtp_attention_biased");
+}
+
+gtp_status gtp_attention_biased_backward(const gtp_attn* a, const gtp_attn_bias* b, const gtp_rows* q,
+                                         const gtp_rows* k, const gtp_rows* v, const gtp_rows* o, const gtp_rows* dout,
+                                         const float* lse, const gtp_rows* dq, const gtp_rows* dk, const gtp_rows* dv,
+                                         float* dbias, void* work, int64_t work_bytes, void* stream) {
+  return attention_backward(a, b, true, q, k, v, o, dout, lse, dq, dk, dv, dbias, work, work_bytes, stream,
+                            "gtp_attention_biased_backward");
 }
 
 }  // extern "C"

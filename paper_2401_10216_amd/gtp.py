@@ -60,6 +60,7 @@ class _Attn(ctypes.Structure):
 _ATTN = struct.Struct("<4i5q3Qf4xdQ")
 _ROWS = "Qqq"
 assert _ATTN.size == ctypes.sizeof(_Attn) and struct.calcsize("<" + _ROWS) == ctypes.sizeof(_Rows)
+_BIAS = struct.Struct("<3Qf2i4x")  # gtp_attn_bias
 _RESIDUAL = struct.Struct("<2i2qif6Q")  # gtp_residual
 _RESIDUAL_STATS = struct.Struct("<4Q")  # gtp_residual_stats
 _RESIDUAL_GRADS = struct.Struct("<8Q")  # gtp_residual_grads
@@ -89,6 +90,10 @@ _SIGS = {
     "gtp_attention_work": (_I64, [_P, _I]),
     "gtp_attention": (_I, [_P, _P, _P, _P, _P, _P, _P, _I64, _P]),
     "gtp_attention_backward": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _P]),
+    "gtp_attention_bias_edges": (_I, [ctypes.c_float, _I, _I, _P]),
+    "gtp_attention_biased_work": (_I64, [_P, _P, _I]),
+    "gtp_attention_biased": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _I64, _P]),
+    "gtp_attention_biased_backward": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _P]),
     "gtp_stream_probe": (_I, [_I, _P, _P, _I64, _P]),
     "gtp_compute_probe": (_I, [_I, _I64, _P, _DP, _P]),
     "gtp_grid_floats": (_I64, [_P, _I]),
@@ -823,6 +828,91 @@ def gtp_attention_backward(q, k, v, o, do, lse, scale=None, q_off=None, k_off=No
         work = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes > 0 else None
     _check(lib_.gtp_attention_backward(a, *r[:5], pl, r[5] if "dq" in need else None, *(r[6:] if keys else (None, None)),
                                        _ptr(work), nbytes, _stream(stream)), lib_)
+    return {n: t for n, t in out.items() if n in need}
+
+
+def gtp_attention_bias_edges(buckets: int, r0: float, per_octave: int = 4) -> list:
+    """The first squared distances of buckets 1 .. buckets - 1 of gtp_attention_biased."""
+    out = (ctypes.c_float * max(buckets - 1, 1))()
+    _check(lib().gtp_attention_bias_edges(r0 * r0, buckets, per_octave, out))
+    return list(out)[:buckets - 1]
+
+
+def _bias(bias, q_pos, k_pos, r0, per_octave, q, k):
+    """Packed gtp_attn_bias."""
+    import torch
+    dev, one = q.device, _f32()
+    if not isinstance(bias, torch.Tensor) or bias.dim() != 2:
+        raise ValueError("bias must be [H, buckets]")
+    pb = _want(bias, "bias", (q.shape[1], bias.shape[1]), one, dev)
+    pq = _want(q_pos, "q_pos", (q.shape[0], 3), one, dev)
+    pk = pq if k_pos is None and k.shape[0] == q.shape[0] else _want(k_pos, "k_pos", (k.shape[0], 3), one, dev)
+    return _BIAS.pack(pb, pq, pk, r0 * r0, bias.shape[1], per_octave)
+
+
+def gtp_attention_biased(q, k, v, bias, q_pos, k_pos=None, r0: float = 1.0, per_octave: int = 4, scale=None, q_off=None,
+                         k_off=None, max_q=None, max_k=None, key_mask=None, p: float = 0.0, rng=None, o=None, lse=None,
+                         stream=None):
+    """gtp_attention with a learned bias[H, buckets] (fp32, up to 64 buckets) added to the scores by the distance of
+    q_pos[Tq, 3] and k_pos[Tk, 3] (fp32; left out: q_pos): bucket 0 below r0, then per_octave (1, 2, 4, 8 or 16) buckets
+    for each doubling of the squared distance, the last one open (gtp_attention_bias_edges names the edges).  -inf gives
+    a bucket's pairs probability zero.  Everything else, and what it returns, as gtp_attention."""
+    import torch
+    desc, rows = _attn(q, k, v, scale, q_off, k_off, max_q, max_k, key_mask, p, rng)
+    b = _bias(bias, q_pos, k_pos, r0, per_octave, q, k)
+    dev, shape = q.device, q.shape
+    with _allocating(stream):
+        o = torch.empty(shape, dtype=q.dtype, device=dev) if o is None else o
+        lse = torch.empty(shape[:2], dtype=torch.float32, device=dev) if lse is None else lse
+        ro = _attn_rows(o, "o", shape, q.dtype, dev)
+        pl = _want(lse, "lse", shape[:2], (torch.float32,), dev)
+        _on_gpu(q, "q")
+        buf, a, r = _packed(desc, (*rows, *ro))
+        lib_ = lib()
+        nbytes = lib_.gtp_attention_biased_work(a, b, 0)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes > 0 else None
+    _check(lib_.gtp_attention_biased(a, b, *r, pl, _ptr(work), nbytes, _stream(stream)), lib_)
+    return o, lse
+
+
+def gtp_attention_biased_backward(q, k, v, bias, q_pos, k_pos, r0, per_octave, o, do, lse, scale=None, q_off=None,
+                                  k_off=None, max_q=None, max_k=None, key_mask=None, p: float = 0.0, rng=None,
+                                  need=("dq", "dk", "dv", "dbias"), dq=None, dk=None, dv=None, stream=None):
+    """Gradients of <do, gtp_attention_biased(q, k, v, bias, ...)[0]>: a dict with the requested keys among dq, dk, dv
+    (dk and dv go together) and dbias[H, buckets] (fp32).  Arguments as the forward had them, o, lse as it returned
+    them; dq, dk, dv: tensors to write to."""
+    import torch
+    desc, rows = _attn(q, k, v, scale, q_off, k_off, max_q, max_k, key_mask, p, rng)
+    b = _bias(bias, q_pos, k_pos, r0, per_octave, q, k)
+    need = set(need)
+    if need - {"dq", "dk", "dv", "dbias"}:
+        raise ValueError(f"unknown gradients {sorted(need - {'dq', 'dk', 'dv', 'dbias'})}")
+    dev, dt, qs, ks = q.device, q.dtype, q.shape, k.shape
+    ro = _attn_rows(o, "o", qs, dt, dev)
+    rdo = _attn_rows(do, "do", qs, dt, dev)
+    pl = _want(lse, "lse", qs[:2], (torch.float32,), dev)
+    keys = "dk" in need or "dv" in need
+    none = (0, 0, 0)
+    with _allocating(stream):
+        out = {}
+        if "dq" in need:
+            out["dq"] = torch.empty(qs, dtype=dt, device=dev) if dq is None else dq
+        if keys:
+            out["dk"] = torch.empty(ks, dtype=dt, device=dev) if dk is None else dk
+            out["dv"] = torch.empty(ks, dtype=dt, device=dev) if dv is None else dv
+        if "dbias" in need:
+            out["dbias"] = torch.empty_like(bias)
+        rdq = _attn_rows(out["dq"], "dq", qs, dt, dev) if "dq" in need else none
+        rdk = _attn_rows(out["dk"], "dk", ks, dt, dev) if keys else none
+        rdv = _attn_rows(out["dv"], "dv", ks, dt, dev) if keys else none
+        _on_gpu(q, "q")
+        buf, a, r = _packed(desc, (*rows, *ro, *rdo, *rdq, *rdk, *rdv))
+        lib_ = lib()
+        nbytes = lib_.gtp_attention_biased_work(a, b, 1)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes > 0 else None
+    _check(lib_.gtp_attention_biased_backward(a, b, *r[:5], pl, r[5] if "dq" in need else None,
+                                              *(r[6:] if keys else (None, None)), _ptr(out.get("dbias")), _ptr(work),
+                                              nbytes, _stream(stream)), lib_)
     return {n: t for n, t in out.items() if n in need}
 
 
