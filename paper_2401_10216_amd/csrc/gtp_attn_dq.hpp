@@ -66,6 +66,11 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
   RowOperands<T, DP, long_rows<T, DP>()> qf, gf;
   qf.load(static_cast<const T*>(a.q.p) + qi * a.q.row + h * a.q.head, there, hi, a.d, a.vec);
   gf.load(static_cast<const T*>(a.dout.p) + qi * a.dout.row + h * a.dout.head, there, hi, a.d, a.vec);
+  // The matrix unit's sums are cut downwards, some 2^-27 of a value's size on average, which a
+  // bucket's sum of a million dS of both signs would show: every other wave has dout with
+  // its sign turned.
+  const float turn = BIAS && ((wave ^ w.tile ^ int(w.b)) & 1) ? -1.0f : 1.0f;
+  if (BIAS && turn < 0.0f) gf.negate();
   // rows without a key, and rows past the end: every exponential is zero
   const float lse = there ? a.lse[qi * a.H + h] : -INFINITY;
   const float ref = lse == -INFINITY ? INFINITY : lse * kLog2e;
@@ -141,8 +146,12 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float p = pow2(BIAS ? s[r] - ref : fmaf(s[r], a.scale2, -ref));
-      const float g = DROP ? Drop::kept(dp[r] * a.keep, keep, r) : dp[r];
-      s[r] = p * (g - delta);
+      if constexpr (BIAS) {
+        s[r] = p * (DROP ? Drop::kept(dp[r] * (a.keep * turn), keep, r) - delta : fmaf(dp[r], turn, -delta));
+      } else {
+        const float g = DROP ? Drop::kept(dp[r] * a.keep, keep, r) : dp[r];
+        s[r] = p * (g - delta);
+      }
     }
     if (!whole) {
       const uint32_t ok = uint32_t(keys) >> (4 * hi);
