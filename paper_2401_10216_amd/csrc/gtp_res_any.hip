@@ -336,10 +336,4 @@ hipError_t launch_residual_any_backward(const ResArgs& a, hipStream_t s) {
   return a.bf16 ? run_any_backward<uint16_t>(a, s) : run_any_backward<float>(a, s);
 }
 
-int64_t residual_work_floats(const ResArgs& a) { return residual_any_floats(a); }
-hipError_t launch_residual_backward(const ResArgs& a, hipStream_t s) {
-  if (a.N == 0) return a.weights() ? launch_residual_sum(a, nullptr, 0, s) : hipSuccess;
-  return launch_residual_any_backward(a, s);
-}
-
 }  // namespace gtp
