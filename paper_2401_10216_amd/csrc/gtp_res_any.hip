@@ -234,10 +234,10 @@ __global__ __launch_bounds__(kThreads) void k_res_weights(const Back<T> b, int64
     }
 }
 
-// The parts' sums, added in order: a workgroup takes 16 columns (l, c) of E1 and E2 at a time
-// (and of F and G, at degree 0), 64 groups of threads every 64th part each, then a tree over
+// The parts' sums, added in order: a workgroup takes 8 columns (l, c) of E1 and E2 at a time
+// (and of F and G, at degree 0), 128 groups of threads every 128th part each, then a tree over
 // the groups.
-constexpr int kSumThreads = 1024, kSumCols = 16;
+constexpr int kSumThreads = 1024, kSumCols = 8;
 __global__ __launch_bounds__(kSumThreads) void k_res_sum(const float* __restrict__ partial, int64_t parts, int L,
                                                          ResWeights w, float* __restrict__ dscale,
                                                          float* __restrict__ dw1, float* __restrict__ db1,
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(kSumThreads) void k_res_sum(const float* __restrict
     const float* const p = partial + (in ? col : 0);
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (in) {
-#pragma unroll 4
+#pragma unroll 8
       for (int64_t i = g; i < parts; i += kSumThreads / kSumCols) {
         s[0] += p[i * all];
         s[1] += p[i * all + cols];

@@ -20,46 +20,128 @@ struct ResLay {
 // The layout of rows in registers; false where a row does not fit them, or has fewer than 8 elements.
 bool residual_layout(const ResArgs& a, bool wide, bool back, ResLay* out);
 
+int64_t res_lds(const ResLay& y, int64_t K, int L, bool back);  // LDS bytes; back: of the gradient
+
 constexpr int kTeamThreads = 256;
 
-// Tables in LDS, a degree's row of C in C | 1: P = scale w1 [L+1], Q = scale w1's shift [C] (zeros without post),
-// W2 [L+1], B2 [C].
-struct ResTables {
-  float *P, *Q, *W2, *B2;
-  __host__ __device__ static int64_t floats(int L, int64_t C) { return 2 * ((L + 1) * (C | 1) + C); }
-  __device__ ResTables(float* lds, int L, int C) {
-    P = lds;
-    Q = P + (L + 1) * (C | 1);
-    W2 = Q + C;
-    B2 = W2 + (L + 1) * (C | 1);
-  }
-  __device__ void load(const ResWeights& w, int L) const {
-    const int C = int(w.C);
-    for (int l = 0; l <= L; ++l)
-      for (int c = threadIdx.x; c < C; c += int(blockDim.x)) {
-        P[l * (C | 1) + c] = w.s(l, c) * w.post_w(l, c);
-        W2[l * (C | 1) + c] = w.pre_w(l, c);
-      }
-    for (int c = threadIdx.x; c < C; c += int(blockDim.x)) {
-      Q[c] = w.s(0, c) * w.post_b(0, c);
-      B2[c] = w.pre_b(0, c);
+// What a thread's places hold: place j of step i is element V t + i A V + j of the row, always of one
+// coefficient (one degree); a step moves it on by A V / K channels.
+template <int V, bool K1>
+struct Spots {
+  int deg[V];
+  uint32_t next;      // bit j: place j's channel is the one behind place 0's (V <= K: at most two)
+  int ch0, j0, ch;    // channel of place 0 at step 0; the place of a degree-0 coefficient (-1: none) and its channel
+  int cpc;            // channels a step moves on by
+  bool on;
+  __device__ __forceinline__ Spots(int A, int K, int t) {
+    on = t < A;
+    cpc = A * V / K;
+    j0 = -1;
+    next = 0;
+    const int first = on ? V * t : 0;
+    ch0 = ch = first / K;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int c = (first + j) / K, k = first + j - c * K;
+      deg[j] = K1 ? 0 : degree_of(k);
+      if (!K1 && c != ch0) next |= 1u << j;
+      if (!K1 && k == 0) j0 = j, ch = c;
     }
   }
+  // v at the places of degree 0, else 0
+  __device__ __forceinline__ float zero(int j, float v) const { return K1 || j == j0 ? v : 0.0f; }
+  // the sum of v at the places of degree 0
+  __device__ __forceinline__ float sum_zero(const float (&v)[V]) const {
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) s = K1 ? s + v[j] : j == j0 ? v[j] : s;
+    return s;
+  }
 };
+
+// Tables in LDS: P = scale w1 and W2 for each element of the row, so that a thread reads those of
+// its V elements at once (from a table by degree and channel, an address and a word each, they took
+// half of the kernels' instructions), then Q = scale's times the first norm's shift and B2 by channel.
+struct ResTables {
+  float *P, *W2, *Q, *B2;
+  __host__ __device__ static int64_t floats(int64_t elements, int64_t channels) { return 2 * (elements + channels); }
+  // elements: NI A V, channels: NI A V / K, of all steps: the row's and what the last step has past them
+  __device__ ResTables(float* lds, int elements, int channels) {
+    P = lds;
+    W2 = P + elements;
+    Q = W2 + elements;
+    B2 = Q + channels;
+  }
+  // The teams deal the steps.  A table's loads all together, none under a condition of its own: one after the other
+  // they took 26 us for rows of 5184 elements.
+  template <int V, int NI, int TEAMS, bool K1>
+  __device__ void load(const ResWeights& w, const Spots<V, K1>& at, int A, int t, int team) const {
+    constexpr int S = (NI + TEAMS - 1) / TEAMS;
+    const int C = int(w.C);
+    float p[S][V], q[S][V];
+    auto channel = [&](int s, int j) { return (K1 ? V * t + j : at.ch0 + int((at.next >> j) & 1u)) + (s * TEAMS + team) * at.cpc; };
+    auto each = [&](auto f) {
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int j = 0; j < V; ++j) f(s, j);
+    };
+    auto times = [&](const float* from, float (&v)[S][V], bool shift) {
+      if (!from) return;
+      each([&](int s, int j) {
+        const int c = channel(s, j);
+        v[s][j] *= from[(shift ? 0 : at.deg[j] * C) + (c < C ? c : C - 1)];
+      });
+    };
+    auto write = [&](float* to, const float (&v)[S][V], bool by_channel) {
+      if (!at.on) return;
+      each([&](int s, int j) {
+        const int i = s * TEAMS + team, c = channel(s, j);
+        if (i >= NI || (by_channel && !K1 && j != at.j0)) return;
+        to[by_channel ? c : i * A * V + V * t + j] = c < C ? v[s][j] : 0.0f;
+      });
+    };
+    each([&](int s, int j) { p[s][j] = q[s][j] = 1.0f; });
+    times(w.scale, p, false);
+    if (w.b1) {  // scale's row of degree 0 times the shift
+      times(w.scale, q, true);
+      times(w.b1, q, true);
+    } else {
+      each([&](int s, int j) { q[s][j] = 0.0f; });
+    }
+    times(w.w1, p, false);
+    write(P, p, false);
+    write(Q, q, true);
+    each([&](int s, int j) { p[s][j] = 1.0f, q[s][j] = w.b2 ? 1.0f : 0.0f; });
+    times(w.w2, p, false);
+    times(w.b2, q, true);
+    write(W2, p, false);
+    write(B2, q, true);
+  }
+};
+
+template <int V>
+__device__ __forceinline__ void read_table(const float* p, float (&o)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; j += 4) {
+    typedef float f4 __attribute__((ext_vector_type(4)));
+    const f4 v = *reinterpret_cast<const f4*>(p + j);
+    o[j] = v[0], o[j + 1] = v[1], o[j + 2] = v[2], o[j + 3] = v[3];
+  }
+}
 
 // What a team's lanes do together.  red: of a workgroup, [A V] (K1: [A]) by place, [slots] at degree 0, [L + 2] results.
 template <int W, int V, bool K1>
 struct Team {
-  const Places<V>& pl;
+  const Spots<V, K1>& pl;
   int A, K, C, L, t;
   float *red, *zero, *stat;
   __device__ int slots() const { return K1 ? A : pl.cpc; }
   __host__ __device__ static int64_t floats(int64_t A, int64_t K, int L) {
     return W ? 0 : (K1 ? 2 * A : A * V + A * V / K) + L + 2;
   }
-  __device__ Team(const Places<V>& p, int A_, int K_, int C_, int L_, int t_, float* lds)
+  __device__ Team(const Spots<V, K1>& p, int A_, int K_, int C_, int L_, int t_, float* lds)
       : pl(p), A(A_), K(K_), C(C_), L(L_), t(t_), red(lds), zero(lds + (K1 ? A_ : A_ * V)), stat(zero + slots()) {}
-  __device__ bool at_zero(int j) const { return K1 || j == pl.j0; }
   // What one lane wrote to LDS is there for the team's others.
   __device__ void meet() const {
     if constexpr (W == 0) {
@@ -144,23 +226,27 @@ struct Team {
   // own, joined with the threads' sums), so that a mean far from zero costs no digits.
   template <int NI, typename F, typename G, typename O>
   __device__ void statistics(F val, G there, float eps, float& mu, float (&r)[V], O out) const {
-    float q[V], s = 0.0f;
+    float q[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) q[j] = 0.0f;
     if (pl.on)
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-          s += at_zero(j) ? val(i, j) : 0.0f;  // zero past the row's end
+        for (int j = 0; j < V; ++j) q[j] += val(i, j);  // zero past the row's end
+    const float s = pl.sum_zero(q);
+#pragma unroll
+    for (int j = 0; j < V; ++j) q[j] = 0.0f;
     auto squares = [&](float about) {
+      float off[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) off[j] = pl.zero(j, about);
       if (pl.on)
 #pragma unroll
         for (int i = 0; i < NI; ++i)
 #pragma unroll
           for (int j = 0; j < V; ++j) {
-            float v = val(i, j);
-            v = at_zero(j) ? (there(i, j) ? v - about : 0.0f) : v;
+            const float v = there(i, j) ? val(i, j) - off[j] : 0.0f;
             q[j] = fmaf(v, v, q[j]);
           }
     };
@@ -238,9 +324,29 @@ struct RowRegs {
     step_fix<false, T, V>(v[NI - 1], (NI - 1) * AV + V * t, R);
   }
   __device__ __forceinline__ float operator()(int i, int j) const { return get<T, V>(v[i], j); }
+  // fp32 rows only: something made of the element in its place
+  __device__ __forceinline__ void set(int i, int j, float f) {
+    if constexpr (sizeof(T) == 4) v[i][j] = f;
+  }
   __device__ __forceinline__ void renewed() {
 #pragma unroll
     for (int i = 0; i < NI; ++i) renew(v[i]);
+  }
+};
+
+// A row's gate: with one coefficient a channel as the row's elements; else C numbers dealt to the team's lanes (NI a
+// lane at most, since K >= V), which put their sigmoids in LDS.
+template <typename T, int V, int NI, bool K1>
+struct RowGate {
+  RowRegs<T, V, NI> row;
+  float own[NI];
+  __device__ __forceinline__ void load(const T* gate, int t, int AV, int C, int lanes) {
+    if constexpr (K1) {
+      row.load(gate, t, AV, C);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) own[i] = ld(gate, t + i * lanes < C ? t + i * lanes : C - 1);
+    }
   }
 };
 
