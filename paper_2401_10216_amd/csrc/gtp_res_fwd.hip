@@ -8,7 +8,7 @@ namespace gtp {
 namespace {
 
 template <typename T, int V, int NI, int W, bool K1>
-__global__ __launch_bounds__(W ? kTeamThreads : 512, W == 0 && NI * V <= 16 ? 4 : 1) void k_res(const ResArgs a, const ResWeights w, int A) {
+__global__ __launch_bounds__(W ? kTeamThreads : 512) void k_res(const ResArgs a, const ResWeights w, int A) {
   // ResTables, then for each team its gate [NI A V / K + 1], then a workgroup's Team
   extern __shared__ __align__(16) float lds[];
   const int L = a.L, K = (L + 1) * (L + 1), C = int(a.C), R = C * K, AV = A * V;
@@ -36,11 +36,11 @@ __global__ __launch_bounds__(W ? kTeamThreads : 512, W == 0 && NI * V <= 16 ? 4 
   constexpr bool FIRST = W > 0 || NI * V < 16;
   if (FIRST) load(int64_t(blockIdx.x) * TEAMS + team);
   tab.template load<V, NI, TEAMS, K1>(w, pl, A, t, team);
-  if (!FIRST) load(int64_t(blockIdx.x) * TEAMS + team);
   __syncthreads();
   for (int64_t n0 = int64_t(blockIdx.x) * TEAMS; n0 < a.N; n0 += stride) {
     const bool mine = n0 + team < a.N;
     const int64_t n = n0 + team;
+    if (!FIRST) load(n);
     av.fix(t, AV, pl.on ? R : 0);
     xv.fix(t, AV, pl.on ? R : 0);
     if (K1 && gate) gv.row.fix(t, AV, pl.on ? R : 0);
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(W ? kTeamThreads : 512, W == 0 && NI * V <= 16 ? 4 
         if (mine) step_store<false, T, V>(static_cast<T*>(a.r) + n * R, i * AV + V * t, R, o);
       }
     }
-    load(n + stride);  // the next row's, in flight meanwhile
+    if (FIRST) load(n + stride);  // the next row's, in flight meanwhile
     float mu2, r2[V];
     us.template statistics<NI>([&](int i, int j) { return rv[i][j]; }, there, a.eps, mu2, r2, [&](int l, float v) {
       if (a.rstd2 && mine) a.rstd2[n * (L + 1) + l] = v;

@@ -76,47 +76,50 @@ struct ResTables {
   // they took 26 us for rows of 5184 elements.
   template <int V, int NI, int TEAMS, bool K1>
   __device__ void load(const ResWeights& w, const Spots<V, K1>& at, int A, int t, int team) const {
-    constexpr int S = (NI + TEAMS - 1) / TEAMS;
+    constexpr int S = (NI + TEAMS - 1) / TEAMS, Z = K1 ? V : 1;
     const int C = int(w.C);
-    float p[S][V], q[S][V];
     auto channel = [&](int s, int j) { return (K1 ? V * t + j : at.ch0 + int((at.next >> j) & 1u)) + (s * TEAMS + team) * at.cpc; };
-    auto each = [&](auto f) {
+    auto times = [&](const float* from, float (&v)[S][V]) {
+      if (!from) return;
 #pragma unroll
       for (int s = 0; s < S; ++s)
 #pragma unroll
-        for (int j = 0; j < V; ++j) f(s, j);
+        for (int j = 0; j < V; ++j) {
+          const int c = channel(s, j);
+          v[s][j] *= from[at.deg[j] * C + (c < C ? c : C - 1)];
+        }
     };
-    auto times = [&](const float* from, float (&v)[S][V], bool shift) {
-      if (!from) return;
-      each([&](int s, int j) {
-        const int c = channel(s, j);
-        v[s][j] *= from[(shift ? 0 : at.deg[j] * C) + (c < C ? c : C - 1)];
-      });
+    auto elements = [&](float* to, const float* one, const float* other) {
+      float v[S][V];
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[s][j] = 1.0f;
+      times(one, v);
+      times(other, v);
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (at.on && s * TEAMS + team < NI)
+            to[(s * TEAMS + team) * A * V + V * t + j] = channel(s, j) < C ? v[s][j] : 0.0f;
     };
-    auto write = [&](float* to, const float (&v)[S][V], bool by_channel) {
-      if (!at.on) return;
-      each([&](int s, int j) {
-        const int i = s * TEAMS + team, c = channel(s, j);
-        if (i >= NI || (by_channel && !K1 && j != at.j0)) return;
-        to[by_channel ? c : i * A * V + V * t + j] = c < C ? v[s][j] : 0.0f;
-      });
+    // by channel: shift times row 0 of `one`
+    auto channels = [&](float* to, const float* shift, const float* one) {
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int j = 0; j < Z; ++j) {
+          const int c = K1 ? channel(s, j) : at.ch + (s * TEAMS + team) * at.cpc, in = c < C ? c : C - 1;
+          float v = 0.0f;
+          if (shift) v = shift[in] * (one ? one[in] : 1.0f);
+          if (at.on && (K1 || at.j0 >= 0) && s * TEAMS + team < NI) to[c] = c < C ? v : 0.0f;
+        }
     };
-    each([&](int s, int j) { p[s][j] = q[s][j] = 1.0f; });
-    times(w.scale, p, false);
-    if (w.b1) {  // scale's row of degree 0 times the shift
-      times(w.scale, q, true);
-      times(w.b1, q, true);
-    } else {
-      each([&](int s, int j) { q[s][j] = 0.0f; });
-    }
-    times(w.w1, p, false);
-    write(P, p, false);
-    write(Q, q, true);
-    each([&](int s, int j) { p[s][j] = 1.0f, q[s][j] = w.b2 ? 1.0f : 0.0f; });
-    times(w.w2, p, false);
-    times(w.b2, q, true);
-    write(W2, p, false);
-    write(B2, q, true);
+    elements(P, w.scale, w.w1);
+    elements(W2, w.w2, nullptr);
+    channels(Q, w.b1, w.scale);
+    channels(B2, w.b2, nullptr);
   }
 };
 
