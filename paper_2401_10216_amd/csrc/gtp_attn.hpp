@@ -33,6 +33,7 @@ struct AttnArgs {
   int H, Hk, G, d;               // query heads, key heads, H / Hk, head length
   int buckets;                   // of the bias
   uint32_t near, far, step;      // bucket of a squared distance: see Buckets
+  uint8_t *bytes, *bytes_k;      // the pairs' buckets made ahead (see bias_bytes), for rows and for keys; null: made at each score
   int splits;                    // parts that a row's keys (or a key's rows) are dealt to
   float scale, scale2;           // of the scores; times log2(e)
   uint32_t threshold;            // 0: nothing is dropped
@@ -43,6 +44,8 @@ struct AttnArgs {
 // Rows (keys in dk, dv) that a workgroup takes, a wave 32: 128, or 64 where no segment has
 // more, so that short ones do not leave half the waves idle.
 inline int rows_a_tile(int64_t most) { return most <= 64 ? 64 : 128; }
+// Tiles of 32 of a segment's longest side in the buckets made ahead: an even number, since kernels take two at a time.
+__host__ __device__ inline int64_t bytes_tiles(int64_t most) { return (most + 63) / 64 * 2; }
 constexpr int kMaxBias = 4096;  // floats of the bias of a key head's query heads, in LDS
 int dq_rows_a_tile(const AttnArgs& a);  // of dq: a bias's sums beside the longest fp32 tiles fit the LDS of 64 rows only
 int attn_padded(int d);  // the head length that the kernels are instantiated at, >= d
@@ -55,6 +58,15 @@ hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t s);
 void launch_attn_fwd_bias(const AttnArgs& a, hipStream_t s);
 void launch_attn_dq_bias(const AttnArgs& a, hipStream_t s);
 void launch_attn_dkv_bias(const AttnArgs& a, hipStream_t s);
+// With the buckets made ahead (gtp_attn_bytes_*.hip).
+void launch_attn_fwd_bytes(const AttnArgs& a, hipStream_t s);
+void launch_attn_dq_bytes(const AttnArgs& a, hipStream_t s);
+void launch_attn_dkv_bytes(const AttnArgs& a, hipStream_t s);
+// Bytes of the buckets of all pairs of a segment's rows and keys, one for each, if they are worth making ahead for every
+// head at once (0: not).
+int64_t bias_bytes(const AttnArgs& a);
+bool bias_bytes_for_keys(const AttnArgs& a);  // whether dk, dv take them too, turned
+hipError_t launch_bias_bytes(const AttnArgs& a, bool keys, hipStream_t s);
 // Workgroups of dq with a bias that work on one key head, floats for what each leaves of
 // dbias and for their sums, and the sum of them all (a.splits: of dq).
 int64_t attn_bias_parts(const AttnArgs& a);

@@ -3,6 +3,6 @@
 
 namespace gtp {
 
-void launch_attn_dkv_bias(const AttnArgs& a, hipStream_t s) { launch_dkv_kernel<true>(a, s); }
+void launch_attn_dkv_bias(const AttnArgs& a, hipStream_t s) { launch_dkv_kernel<kBias>(a, s); }
 
 }  // namespace gtp

@@ -30,7 +30,7 @@ int64_t chunks(int64_t n) { return n <= kChunk ? 1 : (n + kChunk - 1) / kChunk; 
 
 }  // namespace
 
-void launch_attn_dq_bias(const AttnArgs& a, hipStream_t s) { launch_dq_kernel<true>(a, s); }
+void launch_attn_dq_bias(const AttnArgs& a, hipStream_t s) { launch_dq_kernel<kBias>(a, s); }
 
 int64_t attn_bias_parts(const AttnArgs& a) {
   const int64_t BM = dq_rows_a_tile(a);

@@ -3,6 +3,6 @@
 
 namespace gtp {
 
-void launch_attn_fwd_bias(const AttnArgs& a, hipStream_t s) { launch_fwd_kernel<true>(a, s); }
+void launch_attn_fwd_bias(const AttnArgs& a, hipStream_t s) { launch_fwd_kernel<kBias>(a, s); }
 
 }  // namespace gtp

@@ -580,6 +580,23 @@ struct Buckets {
   }
 };
 
+// What the kernels take of a bias.
+constexpr int kNoBias = 0, kBias = 1, kBiasBytes = 2;
+
+// The buckets made ahead: for each segment, block of 32 columns (a wave's: rows or keys, `at` in the segment) and tile of
+// 32 of the other side, a lane's 16 buckets in the order of a result's registers, four times the bucket each: 16 bytes a lane,
+// 1 KB a wave and tile.  blocks, tiles: of a segment.
+__device__ __forceinline__ const u32x4* bucket_bytes(const uint8_t* bytes, int64_t b, int64_t blocks, int64_t tiles,
+                                                     int64_t at, int hi) {
+  return reinterpret_cast<const u32x4*>(bytes) + ((b * blocks + (at >> 5)) * tiles) * 64 + (at & 31) + 32 * hi;
+}
+// The byte of register r.
+__device__ __forceinline__ uint32_t bucket_byte(const u32x4& v, int r) { return (v[r >> 2] >> (8 * (r & 3))) & 0xffu; }
+// The word that lies `byte` bytes behind p.
+__device__ __forceinline__ float word_at(const float* p, uint32_t byte) {
+  return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p) + byte);
+}
+
 // The bias of key head hk's query heads in LDS, in units of log 2: [G][buckets].
 __device__ __forceinline__ void load_bias(const AttnArgs& a, int hk, float* table) {
   const int n = a.G * a.buckets;

@@ -29,19 +29,19 @@ constexpr int dkv_waves() {
 // Workgroup: 32 NW keys of one key head (a wave 32), rows in tiles of 32.  Heads
 // longer than 128 are dealt to `parts` workgroups by output elements (DO each):
 // the accumulators of all of them would not fit the registers.
-template <typename T, int DP, int DO, int RT, bool DROP, bool BIAS, int NW>
+template <typename T, int DP, int DO, int RT, bool DROP, int BIAS, int NW>
 __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(const AttnArgs a, int64_t n_wg, int tiles) {
   constexpr int NT = 64 * NW, BK = 32 * NW, BR = 32 * RT, NC = DP / 16, NDT = DO / 32, PARTS = DP / DO;
   __shared__ __align__(16) char tq[tile_bytes<T, DP, BR>()];
   __shared__ __align__(16) char tg[tile_bytes<T, DP, BR>()];
   __shared__ __align__(16) float t_ref[BR], t_delta[BR];
-  __shared__ __align__(16) int t_head[BIAS ? BR : 4];  // where in `more` the bias of the row's head is
-  extern __shared__ __align__(16) float more[];        // BIAS: positions of the tile's rows [3][BR], the bias [G][buckets]
+  __shared__ __align__(16) int t_head[BIAS == kBias ? BR : 4];  // where in `more` the bias of the row's head is
+  extern __shared__ __align__(16) float more[];        // kBias: positions of the tile's rows [3][BR]; a bias: it [G][buckets]
   lds_poison(reinterpret_cast<float*>(tq), int(sizeof(tq) / 4));
   lds_poison(reinterpret_cast<float*>(tg), int(sizeof(tg) / 4));
   lds_poison(t_ref, BR);
   lds_poison(t_delta, BR);
-  if constexpr (BIAS) lds_poison(reinterpret_cast<float*>(t_head), BR);
+  if constexpr (BIAS == kBias) lds_poison(reinterpret_cast<float*>(t_head), BR);
   const Work w(blockIdx.x, n_wg, tiles * PARTS, a.splits, a.Hk);
   const int tile = w.tile / PARTS, part = w.tile % PARTS;
   int64_t qs, nq, ks, nk;
@@ -63,10 +63,16 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
   Drop drop;
   if constexpr (DROP) drop.init(a, w.b, w.hk);
   float px = 0.0f, py = 0.0f, pz = 0.0f;
-  if constexpr (BIAS) {
-    lds_poison(more, 3 * BR + a.G * a.buckets);
-    load_bias(a, w.hk, more + 3 * BR);  // the loop's barriers stand before its use
-    px = a.k_pos[3 * jc], py = a.k_pos[3 * jc + 1], pz = a.k_pos[3 * jc + 2];
+  constexpr int POS = BIAS == kBias ? 3 * BR : 0;
+  const u32x4* bytes = nullptr;
+  u32x4 ahead[BIAS == kBiasBytes ? RT : 1];
+  if constexpr (BIAS != kNoBias) {
+    lds_poison(more, POS + a.G * a.buckets);
+    load_bias(a, w.hk, more + POS);  // the loop's barriers stand before its use
+    if constexpr (BIAS == kBias)
+      px = a.k_pos[3 * jc], py = a.k_pos[3 * jc + 1], pz = a.k_pos[3 * jc + 2];
+    else
+      bytes = bucket_bytes(a.bytes_k, w.b, bytes_tiles(a.max_k), bytes_tiles(a.max_q), jc - ks, hi);
   }
   const Buckets bucket(a);
 
@@ -90,10 +96,13 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
     const int64_t at = (qs + i) * a.H + w.hk * a.G + g;
     lse = a.lse[at];
     delta = a.delta[at];
-    if constexpr (BIAS) {
+    if constexpr (BIAS == kBias) {
       sp.fetch(a.q_pos, qs + i);
-      head = 3 * BR + g * a.buckets;
+      head = POS + g * a.buckets;
     }
+    if constexpr (BIAS == kBiasBytes)  // one query head a key head: rows are atoms
+#pragma unroll
+      for (int t = 0; t < RT; ++t) ahead[t] = bytes[((r0 >> 5) + t) * 64];
   };
   int64_t r0 = w.split * per * BR;
   constexpr bool AHEAD = !long_rows<T, DP>() && !(sizeof(T) == 2 && DP == 128);  // there the registers hold no more
@@ -109,10 +118,14 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
       const bool in = r0 + threadIdx.x < rows;
       t_ref[threadIdx.x] = !in || lse == -INFINITY ? INFINITY : lse * kLog2e;
       t_delta[threadIdx.x] = in ? delta : 0.0f;
-      if constexpr (BIAS) t_head[threadIdx.x] = head;
+      if constexpr (BIAS == kBias) t_head[threadIdx.x] = head;
     }
-    if constexpr (BIAS) sp.commit(more);
+    if constexpr (BIAS == kBias) sp.commit(more);
     __syncthreads();
+    u32x4 pairs[BIAS == kBiasBytes ? RT : 1];
+    if constexpr (BIAS == kBiasBytes)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) pairs[t] = ahead[t];
     if (AHEAD && r0 + BR < r_end) fetch(r0 + BR);  // in flight while this tile is worked on
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
@@ -129,15 +142,20 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int row = 32 * t + 8 * g + 4 * hi;
+        uint32_t in = 0;
         const f32x4 rf = *reinterpret_cast<const f32x4*>(t_ref + row);
         const f32x4 de = *reinterpret_cast<const f32x4*>(t_delta + row);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int r = 4 * g + i;
           float e;
-          if constexpr (BIAS) {
-            const float b = more[t_head[row + i] + bucket(more[row + i] - px, more[BR + row + i] - py, more[2 * BR + row + i] - pz)];
-            e = pow2(fmaf(s[r], a.scale2, b) - rf[i]);
+          if constexpr (BIAS == kBiasBytes) {
+            e = pow2(fmaf(s[r], a.scale2, word_at(more, bucket_byte(pairs[t], r))) - rf[i]);
+          } else if constexpr (BIAS == kBias) {
+            // four rows of one atom, or two and two, have one distance
+            if (i == 0 || (i == 2 ? (a.G & 3) != 0 : (a.G & 1) != 0))
+              in = bucket(more[row + i] - px, more[BR + row + i] - py, more[2 * BR + row + i] - pz);
+            e = pow2(fmaf(s[r], a.scale2, more[t_head[row + i] + in]) - rf[i]);
           } else {
             e = pow2(fmaf(s[r], a.scale2, -rf[i]));
           }
@@ -184,18 +202,20 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
                      DROP ? a.keep : 1.0f, part * DO, a.d, hi, a.vec);
 }
 
-template <typename T, int DP, bool DROP, bool BIAS>
+template <typename T, int DP, bool DROP, int BIAS>
 void launch_tiles(const AttnArgs& a, hipStream_t s) {
   constexpr int DO = DP > 128 ? DP / 2 : DP, RT = DP * int(sizeof(T)) <= 128 ? 2 : 1;
   const int64_t BK = rows_a_tile(a.max_k), tiles = (a.max_k + BK - 1) / BK, n = tiles * (DP / DO) * a.splits * a.Hk * a.B;
-  const size_t lds = BIAS ? (3 * 32 * RT + size_t(a.G) * a.buckets) * 4 : 0;
-  if (BK == 64)
+  const size_t lds = BIAS ? ((BIAS == kBias ? 3 * 32 * RT : 0) + size_t(a.G) * a.buckets) * 4 : 0;
+  if constexpr (BIAS == kBiasBytes)  // made for long segments only
+    k_attn_dkv<T, DP, DO, RT, DROP, BIAS, 4><<<uint32_t(n), 256, lds, s>>>(a, n, int(tiles));
+  else if (BK == 64)
     k_attn_dkv<T, DP, DO, RT, DROP, BIAS, 2><<<uint32_t(n), 128, lds, s>>>(a, n, int(tiles));
   else
     k_attn_dkv<T, DP, DO, RT, DROP, BIAS, 4><<<uint32_t(n), 256, lds, s>>>(a, n, int(tiles));
 }
 
-template <typename T, int DP, bool BIAS>
+template <typename T, int DP, int BIAS>
 void launch_dkv_tiles(const AttnArgs& a, hipStream_t s) {
   if (a.threshold)
     launch_tiles<T, DP, true, BIAS>(a, s);
@@ -203,7 +223,7 @@ void launch_dkv_tiles(const AttnArgs& a, hipStream_t s) {
     launch_tiles<T, DP, false, BIAS>(a, s);
 }
 
-template <bool BIAS>
+template <int BIAS>
 void launch_dkv_kernel(const AttnArgs& a, hipStream_t s) {
   switch (attn_padded(a.d)) {
     case 32: return a.bf16 ? launch_dkv_tiles<uint16_t, 32, BIAS>(a, s) : launch_dkv_tiles<float, 32, BIAS>(a, s);

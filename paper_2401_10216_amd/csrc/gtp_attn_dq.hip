@@ -37,10 +37,12 @@ hipError_t launch_attn_delta(const AttnArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_attn_dq(const AttnArgs& a, hipStream_t s) {
-  if (a.bias)
+  if (a.bytes)
+    launch_attn_dq_bytes(a, s);
+  else if (a.bias)
     launch_attn_dq_bias(a, s);
   else
-    launch_dq_kernel<false>(a, s);
+    launch_dq_kernel<kNoBias>(a, s);
   return hipGetLastError();
 }
 

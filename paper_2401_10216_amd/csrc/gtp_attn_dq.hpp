@@ -32,27 +32,28 @@ namespace {
 // so the order of its additions, and with it the result, is always the same); at the end the
 // columns of a query head are added, and what the workgroups leave by launch_attn_bias_sum.
 // The LDS's own fp32 addition took 260 cycles a wave: 4051 us where reading and writing takes XXXX.
-template <typename T, int DP, bool DROP, bool BIAS, int NW>
+template <typename T, int DP, bool DROP, int BIAS, int NW>
 __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(const AttnArgs a, int64_t n_wg, int tiles) {
   constexpr int NT = 64 * NW, BM = 32 * NW, BN = 32, NC = DP / 16, NDT = DP / 32;
   __shared__ __align__(16) char tk[tile_bytes<T, DP, BN>()];
   __shared__ __align__(16) char tv[tile_bytes<T, DP, BN>()];
   lds_poison(reinterpret_cast<float*>(tk), int(sizeof(tk) / 4));
   lds_poison(reinterpret_cast<float*>(tv), int(sizeof(tv) / 4));
-  // BIAS: positions of the tile's keys [3][BN], the bias [G][buckets], the lanes' sums [buckets][NT]
+  // kBias: positions of the tile's keys [3][BN]; a bias: it [G][buckets], the lanes' sums [buckets][NT]
   extern __shared__ __align__(16) float more[];
   const Work w(blockIdx.x, n_wg, tiles, a.splits, a.Hk);
   int64_t qs, nq, ks, nk;
   segment(a.q_off, w.b, a.max_q, a.Tq, qs, nq);
   segment(a.k_off, w.b, a.max_k, a.Tk, ks, nk);
   const int64_t rows = nq * a.G;
-  float* const table = more + 3 * BN;
+  constexpr int POS = BIAS == kBias ? 3 * BN : 0;
+  float* const table = more + POS;
   float* const sums = table + a.G * a.buckets;
   float* const left = BIAS && a.dbias ? a.bias_part + (((w.hk * a.B + w.b) * a.splits + w.split) * tiles + w.tile) *
                                                           (int64_t(a.G) * a.buckets)
                                       : nullptr;
   if (int64_t(w.tile) * BM >= rows) {
-    if (BIAS && left)
+    if (left)
       for (int i = threadIdx.x; i < a.G * a.buckets; i += NT) left[i] = 0.0f;
     return;
   }
@@ -82,12 +83,17 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
   if constexpr (DROP) drop.init(a, w.b, w.hk);
 
   float px = 0.0f, py = 0.0f, pz = 0.0f;
-  if constexpr (BIAS) {
-    lds_poison(more, 3 * BN + a.G * a.buckets + (left ? a.buckets * NT : 0));
+  const u32x4* bytes = nullptr;
+  u32x4 ahead;
+  if constexpr (BIAS != kNoBias) {
+    lds_poison(more, POS + a.G * a.buckets + (left ? a.buckets * NT : 0));
     load_bias(a, w.hk, table);  // the loop's barriers stand before its use
     if (left)
       for (int i = 0; i < a.buckets; ++i) sums[i * NT + threadIdx.x] = 0.0f;
-    px = a.q_pos[3 * qi], py = a.q_pos[3 * qi + 1], pz = a.q_pos[3 * qi + 2];
+    if constexpr (BIAS == kBias)
+      px = a.q_pos[3 * qi], py = a.q_pos[3 * qi + 1], pz = a.q_pos[3 * qi + 2];
+    else
+      bytes = bucket_bytes(a.bytes, w.b, bytes_tiles(a.max_q), bytes_tiles(a.max_k), qi - qs, hi);
   }
   const float* const own = table + g * a.buckets;
   const Buckets bucket(a);
@@ -102,10 +108,11 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
   StagedPos<BN> sp;
   auto fetch = [&](int64_t j0) {
     here.fetch(mask, kb, j0, nk, lane);
-    if constexpr (BIAS) {
+    if constexpr (BIAS == kBias) {
       const int64_t j = j0 + (threadIdx.x & (BN - 1));
       sp.fetch(a.k_pos, ks + (j < nk ? j : j0));
     }
+    if constexpr (BIAS == kBiasBytes) ahead = bytes[(j0 >> 5) * 64];
     sk.fetch([&](int r) { return kb + (j0 + r < nk ? j0 + r : j0) * a.k.row; }, a.d, a.vec);
     sv.fetch([&](int r) { return vb + (j0 + r < nk ? j0 + r : j0) * a.v.row; }, a.d, a.vec);
   };
@@ -119,8 +126,10 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
     const uint64_t keys = here.rows(mask, j0, nk, lane);  // zeros stand for absent keys' rows
     sk.commit(tk, a.d, a.vec, whole, keys);
     sv.commit(tv, a.d, a.vec, whole, keys);
-    if constexpr (BIAS) sp.commit(more);
+    if constexpr (BIAS == kBias) sp.commit(more);
     __syncthreads();
+    u32x4 pairs;
+    if constexpr (BIAS == kBiasBytes) pairs = ahead;
     if (AHEAD && j0 + BN < j_end) fetch(j0 + BN);  // in flight while this tile is worked on
     f32x16 s = zero16(), dp = zero16();
 #pragma unroll
@@ -128,8 +137,17 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
       mma2<T>(tile_operand<T, DP, BN>(tk, l31, c, hi), qf(c), s, tile_operand<T, DP, BN>(tv, l31, c, hi), gf(c), dp);
     uint32_t keep = 0xffffu;
     if constexpr (DROP) keep = drop.keys_of_row(R0, j0, lane);
-    uint32_t in[BIAS ? 16 : 1];  // the scores' buckets
-    if constexpr (BIAS) {
+    uint32_t in[BIAS == kBias ? 16 : 1];  // the scores' buckets
+    // where score r's bias, and its lane's sum, are
+    auto bias_at = [&](int r) { return BIAS == kBias ? own[in[r]] : word_at(own, bucket_byte(pairs, r)); };
+    auto sum_at = [&](int r) { return sums + (BIAS == kBias ? in[r] : bucket_byte(pairs, r) >> 2) * NT + threadIdx.x; };
+    auto one_bucket = [&](int r, int k) {
+      return BIAS == kBias ? in[r] == in[k] : bucket_byte(pairs, r) == bucket_byte(pairs, k);
+    };
+    if constexpr (BIAS == kBiasBytes)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale2, bias_at(r));
+    if constexpr (BIAS == kBias) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float* const at = more + 8 * i + 4 * hi;
@@ -139,14 +157,14 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
         for (int j = 0; j < 4; ++j) {
           const int r = 4 * i + j;
           in[r] = bucket(px - x[j], py - y[j], pz - z[j]);
-          s[r] = fmaf(s[r], a.scale2, own[in[r]]);
+          s[r] = fmaf(s[r], a.scale2, bias_at(r));
         }
       }
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float p = pow2(BIAS ? s[r] - ref : fmaf(s[r], a.scale2, -ref));
-      if constexpr (BIAS) {
+      if constexpr (BIAS != kNoBias) {
         s[r] = p * (DROP ? Drop::kept(dp[r] * (a.keep * turn), keep, r) - delta : fmaf(dp[r], turn, -delta));
       } else {
         const float g = DROP ? Drop::kept(dp[r] * a.keep, keep, r) : dp[r];
@@ -158,7 +176,7 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = (ok >> tile_row(r, 0)) & 1u ? s[r] : 0.0f;
     }
-    if constexpr (BIAS) {
+    if constexpr (BIAS != kNoBias) {
       if (left) {
         // four at a time: their words are read together, and where two of them are one word, its
         // last writer adds to what the other writes
@@ -166,13 +184,13 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
         for (int i = 0; i < 4; ++i) {
           float *at[4], v[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) at[j] = sums + in[4 * i + j] * NT + threadIdx.x;
+          for (int j = 0; j < 4; ++j) at[j] = sum_at(4 * i + j);
 #pragma unroll
           for (int j = 0; j < 4; ++j) v[j] = *at[j];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
 #pragma unroll
-            for (int k = 0; k < j; ++k) v[j] = in[4 * i + k] == in[4 * i + j] ? v[k] : v[j];
+            for (int k = 0; k < j; ++k) v[j] = one_bucket(4 * i + k, 4 * i + j) ? v[k] : v[j];
             v[j] += s[4 * i + j];
           }
 #pragma unroll
@@ -183,7 +201,7 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
     const Columns<T> ds(s);
     mma_turned<T, DP, BN>(tk, 0, 0, ds, lane, acc);
   }
-  if constexpr (BIAS) {
+  if constexpr (BIAS != kNoBias) {
     if (left) {
       // which columns count for query head h: rows past the end and empty rows (of which 0 times an infinity may
       // be NaN) count for none
@@ -215,17 +233,19 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
                    hi, a.vec);
 }
 
-template <typename T, int DP, bool DROP, bool BIAS>
+template <typename T, int DP, bool DROP, int BIAS>
 void launch_tiles(const AttnArgs& a, hipStream_t s) {
   const int64_t BM = dq_rows_a_tile(a), tiles = (a.max_q * a.G + BM - 1) / BM, n = tiles * a.splits * a.Hk * a.B;
-  const size_t lds = BIAS ? (3 * 32 + size_t(a.G) * a.buckets + (a.dbias ? size_t(a.buckets) * 2 * BM : 0)) * 4 : 0;
-  if (BM == 64)
+  const size_t lds = BIAS ? ((BIAS == kBias ? 3 * 32 : 0) + size_t(a.G) * a.buckets + (a.dbias ? size_t(a.buckets) * 2 * BM : 0)) * 4 : 0;
+  if constexpr (BIAS == kBiasBytes)  // made for long segments only
+    k_attn_dq<T, DP, DROP, BIAS, 4><<<uint32_t(n), 256, lds, s>>>(a, n, int(tiles));
+  else if (BM == 64)
     k_attn_dq<T, DP, DROP, BIAS, 2><<<uint32_t(n), 128, lds, s>>>(a, n, int(tiles));
   else
     k_attn_dq<T, DP, DROP, BIAS, 4><<<uint32_t(n), 256, lds, s>>>(a, n, int(tiles));
 }
 
-template <typename T, int DP, bool BIAS>
+template <typename T, int DP, int BIAS>
 void launch_dq_tiles(const AttnArgs& a, hipStream_t s) {
   if (a.threshold)
     launch_tiles<T, DP, true, BIAS>(a, s);
@@ -233,7 +253,7 @@ void launch_dq_tiles(const AttnArgs& a, hipStream_t s) {
     launch_tiles<T, DP, false, BIAS>(a, s);
 }
 
-template <bool BIAS>
+template <int BIAS>
 void launch_dq_kernel(const AttnArgs& a, hipStream_t s) {
   switch (attn_padded(a.d)) {
     case 32: return a.bf16 ? launch_dq_tiles<uint16_t, 32, BIAS>(a, s) : launch_dq_tiles<float, 32, BIAS>(a, s);

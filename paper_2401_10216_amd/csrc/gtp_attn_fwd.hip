@@ -180,10 +180,12 @@ void join(const AttnArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t s) {
-  if (a.bias)
+  if (a.bytes)
+    launch_attn_fwd_bytes(a, s);
+  else if (a.bias)
     launch_attn_fwd_bias(a, s);
   else
-    launch_fwd_kernel<false>(a, s);
+    launch_fwd_kernel<kNoBias>(a, s);
   if (a.splits > 1) a.bf16 ? join<uint16_t>(a, s) : join<float>(a, s);
   return hipGetLastError();
 }

@@ -45,14 +45,14 @@ constexpr float kSlack = 8.0f;  // probabilities stay below 2^8: far from overfl
 
 // Workgroup: 32 NW rows of one key head (a wave 32), keys in tiles of 32 KT.  Heads longer
 // than 128 leave the registers room for one wave a SIMD only.
-template <typename T, int DP, int KT, bool DROP, bool BIAS, int NW>
+template <typename T, int DP, int KT, bool DROP, int BIAS, int NW>
 __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const AttnArgs a, int64_t n_wg, int tiles) {
   constexpr int NT = 64 * NW, BM = 32 * NW, BN = 32 * KT, NC = DP / 16, NDT = DP / 32;
   __shared__ __align__(16) char tk[tile_bytes<T, DP, BN>()];
   __shared__ __align__(16) char tv[tile_bytes<T, DP, BN>()];
   lds_poison(reinterpret_cast<float*>(tk), int(sizeof(tk) / 4));
   lds_poison(reinterpret_cast<float*>(tv), int(sizeof(tv) / 4));
-  extern __shared__ __align__(16) float more[];  // BIAS: positions of the tile's keys [3][BN], the bias [G][buckets]
+  extern __shared__ __align__(16) float more[];  // kBias: positions of the tile's keys [3][BN]; a bias: it [G][buckets]
   const Work w(blockIdx.x, n_wg, tiles, a.splits, a.Hk);
   int64_t qs, nq, ks, nk;
   segment(a.q_off, w.b, a.max_q, a.Tq, qs, nq);
@@ -73,11 +73,17 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const A
   if (a.scale2 < 0.0f) qf.negate();
   float px = 0.0f, py = 0.0f, pz = 0.0f;
   const float* table = nullptr;
-  if constexpr (BIAS) {
-    lds_poison(more, 3 * BN + a.G * a.buckets);
-    load_bias(a, w.hk, more + 3 * BN);  // the loop's barriers stand before its use
-    table = more + 3 * BN + g * a.buckets;
-    px = a.q_pos[3 * qi], py = a.q_pos[3 * qi + 1], pz = a.q_pos[3 * qi + 2];
+  constexpr int POS = BIAS == kBias ? 3 * BN : 0;
+  const u32x4* bytes = nullptr;
+  u32x4 ahead[BIAS == kBiasBytes ? KT : 1];
+  if constexpr (BIAS != kNoBias) {
+    lds_poison(more, POS + a.G * a.buckets);
+    load_bias(a, w.hk, more + POS);  // the loop's barriers stand before its use
+    table = more + POS + g * a.buckets;
+    if constexpr (BIAS == kBias)
+      px = a.q_pos[3 * qi], py = a.q_pos[3 * qi + 1], pz = a.q_pos[3 * qi + 2];
+    else
+      bytes = bucket_bytes(a.bytes, w.b, bytes_tiles(a.max_q), bytes_tiles(a.max_k), qi - qs, hi);
   }
   const Buckets bucket(a);
   f32x16 acc[NDT];
@@ -99,10 +105,13 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const A
   StagedPos<BN> sp;
   auto fetch = [&](int64_t j0) {
     here.fetch(mask, kb, j0, nk, lane);
-    if constexpr (BIAS) {
+    if constexpr (BIAS == kBias) {
       const int64_t j = j0 + (threadIdx.x & (BN - 1));
       sp.fetch(a.k_pos, ks + (j < nk ? j : j0));
     }
+    if constexpr (BIAS == kBiasBytes)
+#pragma unroll
+      for (int t = 0; t < KT; ++t) ahead[t] = bytes[((j0 >> 5) + t) * 64];
     sk.fetch([&](int r) { return kb + (j0 + r < nk ? j0 + r : j0) * a.k.row; }, a.d, a.vec);
     sv.fetch([&](int r) { return vb + (j0 + r < nk ? j0 + r : j0) * a.v.row; }, a.d, a.vec);
   };
@@ -116,8 +125,12 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const A
     const uint64_t keys = here.rows(mask, j0, nk, lane);  // zeros stand for absent keys' rows
     sk.commit(tk, a.d, a.vec, whole, keys);
     sv.commit(tv, a.d, a.vec, whole, keys);
-    if constexpr (BIAS) sp.commit(more);
+    if constexpr (BIAS == kBias) sp.commit(more);
     __syncthreads();
+    u32x4 in[BIAS == kBiasBytes ? KT : 1];
+    if constexpr (BIAS == kBiasBytes)
+#pragma unroll
+      for (int t = 0; t < KT; ++t) in[t] = ahead[t];
     if (AHEAD && j0 + BN < j_end) fetch(j0 + BN);  // in flight while this tile is worked on
     f32x16 s[KT];
     uint32_t ok[KT];
@@ -132,7 +145,13 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const A
       else
         mma<T>(tile_operand<T, DP, BN>(tk, l31, c, hi), q, s[0]);
     }
-    if constexpr (BIAS) {  // scores in units of log 2 from here on
+    if constexpr (BIAS == kBiasBytes) {
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = fmaf(s[t][r], scale2, word_at(table, bucket_byte(in[t], r)));
+    }
+    if constexpr (BIAS == kBias) {  // scores in units of log 2 from here on
 #pragma unroll
       for (int t = 0; t < KT; ++t)
 #pragma unroll
@@ -207,18 +226,20 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const A
   if (hi == 0) a.lse[qi * a.H + h] = lse;
 }
 
-template <typename T, int DP, bool DROP, bool BIAS>
+template <typename T, int DP, bool DROP, int BIAS>
 void launch_tiles(const AttnArgs& a, hipStream_t s) {
   constexpr int KT = key_tiles(DP, sizeof(T) == 2);
   const int64_t BM = rows_a_tile(a.max_q * a.G), tiles = (a.max_q * a.G + BM - 1) / BM, n = tiles * a.splits * a.Hk * a.B;
-  const size_t lds = BIAS ? (3 * 32 * KT + size_t(a.G) * a.buckets) * 4 : 0;
-  if (BM == 64)
+  const size_t lds = BIAS ? ((BIAS == kBias ? 3 * 32 * KT : 0) + size_t(a.G) * a.buckets) * 4 : 0;
+  if constexpr (BIAS == kBiasBytes)  // made for long segments only
+    k_attn_fwd<T, DP, KT, DROP, BIAS, 4><<<uint32_t(n), 256, lds, s>>>(a, n, int(tiles));
+  else if (BM == 64)
     k_attn_fwd<T, DP, KT, DROP, BIAS, 2><<<uint32_t(n), 128, lds, s>>>(a, n, int(tiles));
   else
     k_attn_fwd<T, DP, KT, DROP, BIAS, 4><<<uint32_t(n), 256, lds, s>>>(a, n, int(tiles));
 }
 
-template <typename T, int DP, bool BIAS>
+template <typename T, int DP, int BIAS>
 void launch_fwd_tiles(const AttnArgs& a, hipStream_t s) {
   if (a.threshold)
     launch_tiles<T, DP, true, BIAS>(a, s);
@@ -226,7 +247,7 @@ void launch_fwd_tiles(const AttnArgs& a, hipStream_t s) {
     launch_tiles<T, DP, false, BIAS>(a, s);
 }
 
-template <bool BIAS>
+template <int BIAS>
 void launch_fwd_kernel(const AttnArgs& a, hipStream_t s) {
   switch (attn_padded(a.d)) {
     case 32: return a.bf16 ? launch_fwd_tiles<uint16_t, 32, BIAS>(a, s) : launch_fwd_tiles<float, 32, BIAS>(a, s);

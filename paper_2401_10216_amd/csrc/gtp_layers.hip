@@ -411,20 +411,22 @@ gtp_status attn_sizes(const gtp_attn* a, gtp::AttnArgs* g) {
 
 gtp::AttnRows rows_of(const gtp_rows* r) { return r ? gtp::AttnRows{r->data, r->row, r->head} : gtp::AttnRows{}; }
 
-// The forward: the parts of a split call and their lse.  The backward: the rows'
-// deltas, what the workgroups leave of a bias's gradient, then the parts of dq or of dk
-// and dv, one after the other in the same place.
+// The forward: a bias's buckets made ahead, then the parts of a split call and their lse.  The
+// backward: the rows' deltas, what the workgroups leave of a bias's gradient, its buckets (those of
+// the rows, or of the keys, one after the other in the same place), then the parts of dq or of dk and
+// dv, one after the other in the same place.
 int64_t delta_bytes(const gtp::AttnArgs& g) { return (g.Tq * g.H * 4 + 15) / 16 * 16; }
-int64_t bias_bytes(gtp::AttnArgs g) {
+int64_t bias_sum_bytes(gtp::AttnArgs g) {
   if (!g.bias) return 0;
   g.splits = gtp::attn_row_splits(g, true);
   return (gtp::bias_part_floats(g) * 4 + 15) / 16 * 16;
 }
 int64_t attn_work(const gtp::AttnArgs& g, int backward) {
   const int64_t s = gtp::attn_row_splits(g, backward), rows = s > 1 ? s * g.Tq * g.H * (g.d + (backward ? 0 : 1)) * 4 : 0;
-  if (!backward) return rows;
+  const int64_t pairs = gtp::bias_bytes(g);
+  if (!backward) return pairs + rows;
   const int64_t t = gtp::attn_key_splits(g), keys = t > 1 ? 2 * t * g.Tk * g.Hk * g.d * 4 : 0;
-  return delta_bytes(g) + bias_bytes(g) + (rows > keys ? rows : keys);
+  return delta_bytes(g) + bias_sum_bytes(g) + pairs + (rows > keys ? rows : keys);
 }
 
 constexpr float kNearest = 0x1p-100f;
@@ -537,9 +539,16 @@ gtp_status attention(const gtp_attn* a, const gtp_attn_bias* b, bool biased, con
   g.v = rows_of(v);
   g.out = rows_of(o);
   g.lse = lse;
-  g.part = static_cast<float*>(work);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const int64_t pairs = gtp::bias_bytes(g);
+  g.part = reinterpret_cast<float*>(static_cast<char*>(work) + pairs);
   g.splits = gtp::attn_row_splits(g, false);
-  return launched(gtp::launch_attn_fwd(g, static_cast<hipStream_t>(stream)), name);
+  hipError_t e = hipSuccess;
+  if (pairs > 0) {
+    g.bytes = static_cast<uint8_t*>(work);
+    e = gtp::launch_bias_bytes(g, false, st);
+  }
+  return launched(e == hipSuccess ? gtp::launch_attn_fwd(g, st) : e, name);
 }
 
 gtp_status attention_backward(const gtp_attn* a, const gtp_attn_bias* b, bool biased, const gtp_rows* q,
@@ -576,16 +585,26 @@ gtp_status attention_backward(const gtp_attn* a, const gtp_attn_bias* b, bool bi
   hipError_t e = a->B > 0 && a->Tq > 0 ? gtp::launch_attn_delta(g, st) : hipSuccess;
   char* const past = static_cast<char*>(work) + delta_bytes(g);
   g.bias_part = reinterpret_cast<float*>(past);
-  g.part = reinterpret_cast<float*>(past + bias_bytes(g));
+  const int64_t pairs = gtp::bias_bytes(g);
+  uint8_t* const bytes = reinterpret_cast<uint8_t*>(past + bias_sum_bytes(g));
+  g.part = reinterpret_cast<float*>(bytes + pairs);
   if (e == hipSuccess && (dq || dbias) && a->B > 0 && a->max_q > 0) {
     g.splits = gtp::attn_row_splits(g, true);
-    e = gtp::launch_attn_dq(g, st);
+    if (pairs > 0) {
+      g.bytes = bytes;
+      e = gtp::launch_bias_bytes(g, false, st);
+    }
+    if (e == hipSuccess) e = gtp::launch_attn_dq(g, st);
     if (e == hipSuccess && dq && g.splits > 1) e = gtp::launch_attn_sum(g, g.part, g.splits, false, g.out, st);
   }
   if (e == hipSuccess && dbias) e = gtp::launch_attn_bias_sum(g, st);
   if (e == hipSuccess && dk && a->B > 0 && a->max_k > 0) {
     g.splits = gtp::attn_key_splits(g);
-    e = gtp::launch_attn_dkv(g, st);
+    if (pairs > 0 && gtp::bias_bytes_for_keys(g)) {
+      g.bytes_k = bytes;
+      e = gtp::launch_bias_bytes(g, true, st);
+    }
+    if (e == hipSuccess) e = gtp::launch_attn_dkv(g, st);
     const int64_t one = g.splits * g.Tk * g.Hk * g.d;
     if (e == hipSuccess && g.splits > 1) e = gtp::launch_attn_sum(g, g.part, g.splits, true, g.dk, st);
     if (e == hipSuccess && g.splits > 1) e = gtp::launch_attn_sum(g, g.part + one, g.splits, true, g.dv, st);

@@ -97,6 +97,10 @@ CASES = [
     ([511], [513], 1, 1, 48, 0.5, 0, dict(r0=0.5)), ([1025], [1023], 2, 2, 40, 0, 0, dict(box=9.0)), ([31], [700], 12, 4, 24, 0.9, 0.5, {}),
     ([2000], [3], 3, 1, 64, 0, 0, {}), ([1500], [40], 4, 2, 96, 0.2, 0.1, dict(buckets=7)), ([3], [4], 1, 1, 217, 0, 0, {}),
     ([90, 60], [90, 60], 4, 4, 36, 0, 0, dict(cutoff=True, buckets=8, per=2, box=6.0)),
+    # buckets made ahead: long segments, four heads and more
+    ([600, 433], [600, 433], 4, 4, 64, 0, 0, dict(buckets=64, per=8, box=9.0)), ([300, 511], [520, 400], 8, 4, 72, 0.2, 0.1, {}),
+    ([289], [1000], 4, 1, 120, 0, 0, dict(cutoff=True)), ([700], [545], 4, 4, 32, 0.5, 0, {}), ([513], [257], 6, 2, 190, 0, 0.1, {}),
+    ([300], [300], 4, 4, 250, 0.1, 0, dict(buckets=64)), ([401, 0, 399], [0, 300, 390], 4, 4, 96, 0, 0, {}),
     ([20], [500], 64, 1, 16, 0, 0, dict(buckets=64)), ([9], [40], 37, 1, 20, 0, 0.2, dict(buckets=5)),
 ]
 
@@ -331,7 +335,8 @@ def everything(dtype):
     for ql, kl, H, Hk, d, p, more in (([30, 49], [30, 49], 4, 4, 72, 0.1, {}), ([300], [300], 4, 2, 64, 0.0, dict(buckets=64)),
                                       ([2], [4000], 4, 2, 64, 0.0, {}), ([3000], [9], 2, 1, 128, 0.1, {}),
                                       ([90], [80], 2, 2, 160, 0.0, dict(buckets=64)), ([200], [200], 2, 1, 250, 0.0, dict(buckets=64)),
-                                      ([700], [700], 8, 2, 32, 0.0, dict(buckets=3))):
+                                      ([700], [700], 8, 2, 32, 0.0, dict(buckets=3)),
+                                      ([400, 301], [400, 301], 4, 4, 72, 0.1, dict(buckets=64))):
         c = Biased(dtype, ql, kl, H, Hk, d, 0.1, p, **more)
         o, lse = c.forward()
         out += [o, lse, *c.backward(o, lse).values()]

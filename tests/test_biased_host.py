@@ -76,14 +76,18 @@ def test_refusals():
 
 
 def test_work_holds_what_every_workgroup_leaves():
-    """The gradient's work is larger than without a bias by a table for each tile of query rows at least."""
+    """The gradient's work is larger than without a bias by a table for each tile of query rows at least; where the
+    buckets are made ahead, both directions' by a byte a pair."""
     lib = gtp.lib()
     for H, Hk, B, n in ((4, 2, 2, 60), (8, 8, 64, 49), (16, 4, 2, 4300), (8, 2, 1, 1)):
         a = attn_desc(H=H, Hk=Hk, B=B, Tq=B * n, Tk=B * n, max_q=n, max_k=n)
         plain = lib.gtp_attention_work(ctypes.byref(a), 1)
         extra = lib.gtp_attention_biased_work(ctypes.byref(a), bias_desc(), 1) - plain
         assert extra >= B * -(-(n * H // Hk) // 128) * H * 32 * 4
-        assert lib.gtp_attention_biased_work(ctypes.byref(a), bias_desc(), 0) == lib.gtp_attention_work(ctypes.byref(a), 0)
+        pairs = B * n * n if H >= 4 and n > 256 else 0
+        assert extra >= pairs
+        more = lib.gtp_attention_biased_work(ctypes.byref(a), bias_desc(), 0) - lib.gtp_attention_work(ctypes.byref(a), 0)
+        assert pairs <= more <= 1.1 * pairs
 
 
 @pytest.mark.parametrize("buckets,r0,per", [(1, 1.0, 4), (2, 1.0, 1), (3, 0.7, 16), (32, 1.3, 4), (64, 2.0 ** -50, 1), (64, 3.7, 8)])
