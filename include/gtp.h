@@ -488,8 +488,8 @@ typedef struct {
 gtp_status gtp_attention_bias_edges(float r0sq, int buckets, int per_octave, float *edges);
 
 /* gtp_attention with a bias: s = scale q k^T + bias[h, bucket] (b: not NULL; the bias's values are
- * multiplied by log2(e), within fp32's range).  GTP_ERR_UNSUPPORTED where the query heads of a key head
- * have more than 4096 biases in all.  Else as gtp_attention. */
+ * multiplied by log2(e), within fp32's range).  GTP_ERR_UNSUPPORTED where a key head has more than 256
+ * query heads, or they have more than 4096 biases in all.  Else as gtp_attention. */
 int64_t gtp_attention_biased_work(const gtp_attn *a, const gtp_attn_bias *b, int backward);
 gtp_status gtp_attention_biased(const gtp_attn *a, const gtp_attn_bias *b, const gtp_rows *q, const gtp_rows *k,
                                 const gtp_rows *v, const gtp_rows *o, float *lse, void *work, int64_t work_bytes,

@@ -46,7 +46,9 @@ struct AttnArgs {
 inline int rows_a_tile(int64_t most) { return most <= 64 ? 64 : 128; }
 // Tiles of 32 of a segment's longest side in the buckets made ahead: an even number, since kernels take two at a time.
 __host__ __device__ inline int64_t bytes_tiles(int64_t most) { return (most + 63) / 64 * 2; }
-constexpr int kMaxBias = 4096;  // floats of the bias of a key head's query heads, in LDS
+constexpr int kMaxBias = 4096, kMaxBiasHeads = 256;  // of the bias of a key head's query heads, in LDS
+// From one head's to the next: odd, so that heads that share a distance (lanes side by side) read different banks.
+__host__ __device__ inline int bias_stride(int buckets) { return buckets | 1; }
 int dq_rows_a_tile(const AttnArgs& a);  // of dq: a bias's sums beside the longest fp32 tiles fit the LDS of 64 rows only
 int attn_padded(int d);  // the head length that the kernels are instantiated at, >= d
 // Parts that the keys of each row (the rows of each key) are dealt to: 1 where the

@@ -597,11 +597,11 @@ __device__ __forceinline__ float word_at(const float* p, uint32_t byte) {
   return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p) + byte);
 }
 
-// The bias of key head hk's query heads in LDS, in units of log 2: [G][buckets].
+// The bias of key head hk's query heads in LDS, in units of log 2: [G][bias_stride].
 __device__ __forceinline__ void load_bias(const AttnArgs& a, int hk, float* table) {
-  const int n = a.G * a.buckets;
+  const int n = a.G * a.buckets, stride = bias_stride(a.buckets);
   const float* const from = a.bias + int64_t(hk) * n;
-  for (int i = threadIdx.x; i < n; i += int(blockDim.x)) table[i] = from[i] * kLog2e;
+  for (int i = threadIdx.x; i < n; i += int(blockDim.x)) table[i / a.buckets * stride + i % a.buckets] = from[i] * kLog2e;
 }
 
 // Positions of a tile's rows, one after the other x, y, z [ROWS] each in LDS: a lane fetches row lane % ROWS's.

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
   __shared__ __align__(16) char tg[tile_bytes<T, DP, BR>()];
   __shared__ __align__(16) float t_ref[BR], t_delta[BR];
   __shared__ __align__(16) int t_head[BIAS == kBias ? BR : 4];  // where in `more` the bias of the row's head is
-  extern __shared__ __align__(16) float more[];        // kBias: positions of the tile's rows [3][BR]; a bias: it [G][buckets]
+  extern __shared__ __align__(16) float more[];        // kBias: positions of the tile's rows [3][BR]; a bias: it [G][bias_stride]
   lds_poison(reinterpret_cast<float*>(tq), int(sizeof(tq) / 4));
   lds_poison(reinterpret_cast<float*>(tg), int(sizeof(tg) / 4));
   lds_poison(t_ref, BR);
@@ -67,7 +67,7 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
   const u32x4* bytes = nullptr;
   u32x4 ahead[BIAS == kBiasBytes ? RT : 1];
   if constexpr (BIAS != kNoBias) {
-    lds_poison(more, POS + a.G * a.buckets);
+    lds_poison(more, POS + a.G * bias_stride(a.buckets));
     load_bias(a, w.hk, more + POS);  // the loop's barriers stand before its use
     if constexpr (BIAS == kBias)
       px = a.k_pos[3 * jc], py = a.k_pos[3 * jc + 1], pz = a.k_pos[3 * jc + 2];
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
     delta = a.delta[at];
     if constexpr (BIAS == kBias) {
       sp.fetch(a.q_pos, qs + i);
-      head = POS + g * a.buckets;
+      head = POS + g * bias_stride(a.buckets);
     }
     if constexpr (BIAS == kBiasBytes)  // one query head a key head: rows are atoms
 #pragma unroll
@@ -142,7 +142,10 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int row = 32 * t + 8 * g + 4 * hi;
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
         uint32_t in = 0;
+        i32x4 head_at = {0, 0, 0, 0};
+        if constexpr (BIAS == kBias) head_at = *reinterpret_cast<const i32x4*>(t_head + row);
         const f32x4 rf = *reinterpret_cast<const f32x4*>(t_ref + row);
         const f32x4 de = *reinterpret_cast<const f32x4*>(t_delta + row);
 #pragma unroll
@@ -155,7 +158,7 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
             // four rows of one atom, or two and two, have one distance
             if (i == 0 || (i == 2 ? (a.G & 3) != 0 : (a.G & 1) != 0))
               in = bucket(more[row + i] - px, more[BR + row + i] - py, more[2 * BR + row + i] - pz);
-            e = pow2(fmaf(s[r], a.scale2, more[t_head[row + i] + in]) - rf[i]);
+            e = pow2(fmaf(s[r], a.scale2, more[head_at[i] + in]) - rf[i]);
           } else {
             e = pow2(fmaf(s[r], a.scale2, -rf[i]));
           }
@@ -206,7 +209,7 @@ template <typename T, int DP, bool DROP, int BIAS>
 void launch_tiles(const AttnArgs& a, hipStream_t s) {
   constexpr int DO = DP > 128 ? DP / 2 : DP, RT = DP * int(sizeof(T)) <= 128 ? 2 : 1;
   const int64_t BK = rows_a_tile(a.max_k), tiles = (a.max_k + BK - 1) / BK, n = tiles * (DP / DO) * a.splits * a.Hk * a.B;
-  const size_t lds = BIAS ? ((BIAS == kBias ? 3 * 32 * RT : 0) + size_t(a.G) * a.buckets) * 4 : 0;
+  const size_t lds = BIAS ? ((BIAS == kBias ? 3 * 32 * RT : 0) + size_t(a.G) * bias_stride(a.buckets)) * 4 : 0;
   if constexpr (BIAS == kBiasBytes)  // made for long segments only
     k_attn_dkv<T, DP, DO, RT, DROP, BIAS, 4><<<uint32_t(n), 256, lds, s>>>(a, n, int(tiles));
   else if (BK == 64)

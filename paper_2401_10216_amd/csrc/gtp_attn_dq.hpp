@@ -21,6 +21,7 @@
 #pragma once
 
 #include "gtp_attn_core.hpp"
+#include "gtp_norm_core.hpp"
 
 namespace gtp {
 namespace {
@@ -39,7 +40,7 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
   __shared__ __align__(16) char tv[tile_bytes<T, DP, BN>()];
   lds_poison(reinterpret_cast<float*>(tk), int(sizeof(tk) / 4));
   lds_poison(reinterpret_cast<float*>(tv), int(sizeof(tv) / 4));
-  // kBias: positions of the tile's keys [3][BN]; a bias: it [G][buckets], the lanes' sums [buckets][NT]
+  // kBias: positions of the tile's keys [3][BN]; a bias: it [G][bias_stride], the lanes' sums [buckets][NT]
   extern __shared__ __align__(16) float more[];
   const Work w(blockIdx.x, n_wg, tiles, a.splits, a.Hk);
   int64_t qs, nq, ks, nk;
@@ -48,7 +49,7 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
   const int64_t rows = nq * a.G;
   constexpr int POS = BIAS == kBias ? 3 * BN : 0;
   float* const table = more + POS;
-  float* const sums = table + a.G * a.buckets;
+  float* const sums = table + a.G * bias_stride(a.buckets);
   float* const left = BIAS && a.dbias ? a.bias_part + (((w.hk * a.B + w.b) * a.splits + w.split) * tiles + w.tile) *
                                                           (int64_t(a.G) * a.buckets)
                                       : nullptr;
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
   const u32x4* bytes = nullptr;
   u32x4 ahead;
   if constexpr (BIAS != kNoBias) {
-    lds_poison(more, POS + a.G * a.buckets + (left ? a.buckets * NT : 0));
+    lds_poison(more, POS + a.G * bias_stride(a.buckets) + (left ? a.buckets * NT : 0));
     load_bias(a, w.hk, table);  // the loop's barriers stand before its use
     if (left)
       for (int i = 0; i < a.buckets; ++i) sums[i * NT + threadIdx.x] = 0.0f;
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
     else
       bytes = bucket_bytes(a.bytes, w.b, bytes_tiles(a.max_q), bytes_tiles(a.max_k), qi - qs, hi);
   }
-  const float* const own = table + g * a.buckets;
+  const float* const own = table + g * bias_stride(a.buckets);
   const Buckets bucket(a);
 
   const T* const kb = static_cast<const T*>(a.k.p) + ks * a.k.row + w.hk * a.k.head;
@@ -140,7 +141,10 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
     uint32_t in[BIAS == kBias ? 16 : 1];  // the scores' buckets
     // where score r's bias, and its lane's sum, are
     auto bias_at = [&](int r) { return BIAS == kBias ? own[in[r]] : word_at(own, bucket_byte(pairs, r)); };
-    auto sum_at = [&](int r) { return sums + (BIAS == kBias ? in[r] : bucket_byte(pairs, r) >> 2) * NT + threadIdx.x; };
+    auto sum_at = [&](int r) {
+      return reinterpret_cast<float*>(reinterpret_cast<char*>(sums + threadIdx.x) +
+                                      (BIAS == kBias ? 4 * in[r] : bucket_byte(pairs, r)) * NT);
+    };
     auto one_bucket = [&](int r, int k) {
       return BIAS == kBias ? in[r] == in[k] : bucket_byte(pairs, r) == bucket_byte(pairs, k);
     };
@@ -214,8 +218,7 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
           float v = 0.0f;
 #pragma unroll
           for (int i = 0; i < NW; ++i) v += of[64 * i + lane] == h0 ? sums[b * NT + 64 * i + lane] : 0.0f;
-#pragma unroll
-          for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+          v = wave_sum(v);
           if (lane == 0) left[h0 * a.buckets + b] = v;
         }
     }
@@ -236,7 +239,7 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
 template <typename T, int DP, bool DROP, int BIAS>
 void launch_tiles(const AttnArgs& a, hipStream_t s) {
   const int64_t BM = dq_rows_a_tile(a), tiles = (a.max_q * a.G + BM - 1) / BM, n = tiles * a.splits * a.Hk * a.B;
-  const size_t lds = BIAS ? ((BIAS == kBias ? 3 * 32 : 0) + size_t(a.G) * a.buckets + (a.dbias ? size_t(a.buckets) * 2 * BM : 0)) * 4 : 0;
+  const size_t lds = BIAS ? ((BIAS == kBias ? 3 * 32 : 0) + size_t(a.G) * bias_stride(a.buckets) + (a.dbias ? size_t(a.buckets) * 2 * BM : 0)) * 4 : 0;
   if constexpr (BIAS == kBiasBytes)  // made for long segments only
     k_attn_dq<T, DP, DROP, BIAS, 4><<<uint32_t(n), 256, lds, s>>>(a, n, int(tiles));
   else if (BM == 64)

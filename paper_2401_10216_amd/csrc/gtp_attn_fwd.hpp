@@ -52,7 +52,7 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const A
   __shared__ __align__(16) char tv[tile_bytes<T, DP, BN>()];
   lds_poison(reinterpret_cast<float*>(tk), int(sizeof(tk) / 4));
   lds_poison(reinterpret_cast<float*>(tv), int(sizeof(tv) / 4));
-  extern __shared__ __align__(16) float more[];  // kBias: positions of the tile's keys [3][BN]; a bias: it [G][buckets]
+  extern __shared__ __align__(16) float more[];  // kBias: positions of the tile's keys [3][BN]; a bias: it [G][bias_stride]
   const Work w(blockIdx.x, n_wg, tiles, a.splits, a.Hk);
   int64_t qs, nq, ks, nk;
   segment(a.q_off, w.b, a.max_q, a.Tq, qs, nq);
@@ -77,9 +77,9 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const A
   const u32x4* bytes = nullptr;
   u32x4 ahead[BIAS == kBiasBytes ? KT : 1];
   if constexpr (BIAS != kNoBias) {
-    lds_poison(more, POS + a.G * a.buckets);
+    lds_poison(more, POS + a.G * bias_stride(a.buckets));
     load_bias(a, w.hk, more + POS);  // the loop's barriers stand before its use
-    table = more + POS + g * a.buckets;
+    table = more + POS + g * bias_stride(a.buckets);
     if constexpr (BIAS == kBias)
       px = a.q_pos[3 * qi], py = a.q_pos[3 * qi + 1], pz = a.q_pos[3 * qi + 2];
     else
@@ -230,7 +230,7 @@ template <typename T, int DP, bool DROP, int BIAS>
 void launch_tiles(const AttnArgs& a, hipStream_t s) {
   constexpr int KT = key_tiles(DP, sizeof(T) == 2);
   const int64_t BM = rows_a_tile(a.max_q * a.G), tiles = (a.max_q * a.G + BM - 1) / BM, n = tiles * a.splits * a.Hk * a.B;
-  const size_t lds = BIAS ? ((BIAS == kBias ? 3 * 32 * KT : 0) + size_t(a.G) * a.buckets) * 4 : 0;
+  const size_t lds = BIAS ? ((BIAS == kBias ? 3 * 32 * KT : 0) + size_t(a.G) * bias_stride(a.buckets)) * 4 : 0;
   if constexpr (BIAS == kBiasBytes)  // made for long segments only
     k_attn_fwd<T, DP, KT, DROP, BIAS, 4><<<uint32_t(n), 256, lds, s>>>(a, n, int(tiles));
   else if (BM == 64)

@@ -457,7 +457,8 @@ const char* bias_numbers_why(float r0sq, int buckets, int per_octave) {
 gtp_status bias_args(const gtp_attn_bias* b, gtp::AttnArgs* g) {
   if (!b) return bad("NULL description of the bias");
   if (const char* why = bias_numbers_why(b->r0sq, b->buckets, b->per_octave)) return bad(why);
-  if (int64_t(g->G) * b->buckets > gtp::kMaxBias) return unsupported("more than 4096 biases for a key head's query heads");
+  if (g->G > gtp::kMaxBiasHeads || g->G * b->buckets > gtp::kMaxBias)
+    return unsupported("more than 256 query heads, or 4096 biases of them, for a key head");
   if (!b->bias || (!b->q_pos && g->Tq > 0) || (!b->k_pos && g->Tk > 0)) return bad("NULL data pointer");
   if (!aligned(b->bias, 4) || !aligned(b->q_pos, 4) || !aligned(b->k_pos, 4)) return bad("misaligned pointer");
   g->bias = b->bias;

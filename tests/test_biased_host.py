@@ -71,6 +71,7 @@ def test_refusals():
     assert lib.gtp_attention_biased_work(None, b, 0) == -1
     # the query heads of a key head have 65 x 64 biases
     assert fwd(H=130, Hk=2, buckets=64) == UNSUPPORTED
+    assert fwd(H=514, Hk=2, buckets=1) == UNSUPPORTED
     assert fwd(d=257) == UNSUPPORTED
     assert fwd(B=0, Tq=0, Tk=0, max_q=0, max_k=0, q_pos=None, k_pos=None) == OK
 
