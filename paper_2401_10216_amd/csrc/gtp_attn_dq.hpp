@@ -182,21 +182,25 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
     }
     if constexpr (BIAS != kNoBias) {
       if (left) {
-        // four at a time: their words are read together, and where two of them are one word, its
-        // last writer adds to what the other writes
+        // four at a time: their words are read together, and where two of them are one word, the
+        // last one's writer adds them all (first together: a word is larger than what comes to it, and
+        // one rounding at its size instead of four halves their error)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float *at[4], v[4];
+          float *at[4], v[4], u[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) at[j] = sum_at(4 * i + j);
 #pragma unroll
           for (int j = 0; j < 4; ++j) v[j] = *at[j];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
+            float before = 0.0f;
 #pragma unroll
-            for (int k = 0; k < j; ++k) v[j] = one_bucket(4 * i + k, 4 * i + j) ? v[k] : v[j];
-            v[j] += s[4 * i + j];
+            for (int k = 0; k < j; ++k) before = one_bucket(4 * i + k, 4 * i + j) ? u[k] : before;
+            u[j] = before + s[4 * i + j];
           }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] += u[j];
 #pragma unroll
           for (int j = 0; j < 4; ++j) *at[j] = v[j];
         }

@@ -28,13 +28,36 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
   return s;
 }
 
+// q / d for 0 <= q < 2^31 without a division.
+struct Divide {
+  uint32_t d, inv;
+  __device__ __forceinline__ explicit Divide(uint32_t d_) : d(d_), inv(d_ > 1 ? 0xffffffffu / d_ : 0) {}
+  __device__ __forceinline__ uint32_t operator()(uint32_t q) const {
+    if (d == 1) return q;
+    uint32_t n = __umulhi(q, inv);  // at most two too few
+    uint32_t r = q - n * d;
+    if (r >= d) ++n, r -= d;
+    return r >= d ? n + 1 : n;
+  }
+};
+
 // f(channel, element) over a degree's elements of the row at `base`, dealt to the threads.
 template <typename F>
 __device__ __forceinline__ void over_degree(int64_t base, int64_t C, int64_t K, int l, F f) {
-  const int64_t M = 2 * l + 1;
-  for (int64_t q = threadIdx.x; q < C * M; q += kThreads) {
-    const int64_t c = q / M;
-    f(c, base + c * K + l * l + (q - c * M));
+  const int64_t M = 2 * l + 1, at = base + l * l;
+  const Divide by{uint32_t(M)};
+  if (C * M < (int64_t(1) << 31) - kThreads) {  // 64-bit divisions took longer than all else
+    const int n = int(C * M);
+#pragma unroll 4
+    for (int q = threadIdx.x; q < n; q += kThreads) {
+      const uint32_t c = by(uint32_t(q));
+      f(int64_t(c), at + int64_t(c) * K + (q - int(c * uint32_t(M))));
+    }
+  } else {
+    for (int64_t q = threadIdx.x; q < C * M; q += kThreads) {
+      const int64_t c = q / M;
+      f(c, at + c * K + (q - c * M));
+    }
   }
 }
 
@@ -212,8 +235,10 @@ __global__ __launch_bounds__(kThreads) void k_res_weights(const Back<T> b, int64
     for (int l = 0; l <= L; ++l) {
       const int64_t M = 2 * l + 1;
       float e1 = 0.0f, e2 = 0.0f, f = 0.0f, g = 0.0f;
+      const Divide by{uint32_t(M)};
       for (int64_t q = threadIdx.x; q < rows * M; q += kThreads) {
-        const int64_t k = q / M, n = n0 + k, i = (n * C + c) * K + l * l + (q - k * M);
+        const int64_t k = q < (int64_t(1) << 31) ? by(uint32_t(q)) : q / M;
+        const int64_t n = n0 + k, i = (n * C + c) * K + l * l + (q - k * M);
         const float u = b.d(n, l, c, i) * b.open(n, c), d = ld(b.dh, i);
         e1 = fmaf(u, b.xh1(n, l, i), e1);
         e2 = fmaf(d, b.xh2(n, l, i), e2);

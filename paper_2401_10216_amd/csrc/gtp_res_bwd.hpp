@@ -284,7 +284,7 @@ struct Backward {
   hipError_t operator()() const {
     const size_t lds = size_t(res_lds(y, int64_t(a.L + 1) * (a.L + 1), a.L, true));
     auto k = k_res_backward<T, V, NI, W, K1, kTeamThreads>;
-    if constexpr (W == 0 && NI <= 4)
+    if constexpr (W == 0)
       if (y.threads > kTeamThreads) k = k_res_backward<T, V, NI, W, K1, 512>;
     k<<<uint32_t(res_grid(a.N, y)), y.threads, lds, s>>>(a, ResWeights(a), y.A, a.weights() ? a.work : nullptr);
     return hipGetLastError();

@@ -172,14 +172,14 @@ bool residual_layout(const ResArgs& a, bool wide, bool back, ResLay* out) {
   double best = 0.0;
   for (int64_t threads : {256, 512}) {
     const int64_t A = threads / unit * unit, steps = A ? (R + A * V - 1) / (A * V) : 0;
-    if (A == 0 || steps > 32 / V || (back && threads > kTeamThreads && steps > 4)) continue;
+    if (A == 0 || steps > 32 / V) continue;
     const ResLay y{0, V, int(steps), int(A), int(threads)};
     // the share of lanes and steps at work, less where a workgroup's registers leave the CU no second one (of 256
     // threads; of 512, no second wave on a SIMD): 6272 elements, fp32, backward: 355 us on 512 threads in 4 steps, 450 on 256
     // in 7; bf16, forward: 383 on 512 in 2 steps of 8, 473 on 256 in 4
     const int64_t few = back ? (threads > kTeamThreads ? 4 : 3) : (threads > kTeamThreads ? 16 : 20) / V;
     const double use = double(R) / (double(threads) * V * double(steps)) *
-                       (threads > kTeamThreads ? 0.95 : 1.0) * (steps <= few ? 1.0 : 0.75);
+                       (threads > kTeamThreads ? 0.95 : 1.0) * (steps <= few ? 1.0 : back && threads > kTeamThreads ? 0.5 : 0.75);
     if (use > best * 1.02 && fits(y)) best = use, *out = y;
   }
   return best > 0.0;
