@@ -23,7 +23,7 @@ LIB = os.path.join(PKG, "libgtp.so")
 
 HIP_SOURCES = ["gtp_api.hip", "gtp_small.hip", "gtp_wave.hip", "gtp_mfma.hip", "gtp_generic.hip", "gtp_escn.hip",
                "gtp_escn_wave.hip", "gtp_mix.hip", "gtp_mixq.hip", "gtp_probe.hip", "gtp_wgrad.hip", "gtp_wbwd.hip",
-               "gtp_layers.hip", "gtp_norm.hip", "gtp_res_any.hip", "gtp_res_fwd.hip", "gtp_res_bwd.hip",
+               "gtp_layers.hip", "gtp_norm.hip", "gtp_res_any.hip", "gtp_res_long.hip", "gtp_res_fwd.hip", "gtp_res_bwd.hip",
                "gtp_res_bwd_bf16.hip", "gtp_drop.hip", "gtp_attn_fwd.hip", "gtp_attn_dq.hip", "gtp_attn_dkv.hip",
                "gtp_attn_bias_fwd.hip", "gtp_attn_bias_dq.hip", "gtp_attn_bias_dkv.hip", "gtp_attn_bytes.hip",
                "gtp_attn_bytes_fwd.hip", "gtp_attn_bytes_dq.hip", "gtp_attn_bytes_dkv.hip"]

@@ -40,6 +40,12 @@ __host__ __device__ inline int64_t res_columns(int L, int64_t C) { return 2 * in
 // Adds `parts` parts of the weight sums, in order, and makes the weights' gradients.
 hipError_t launch_residual_sum(const ResArgs& a, const float* partial, int64_t parts, hipStream_t s);
 
+// Rows too long for the registers (gtp_res_long.hip), where residual_is_long says so.
+bool residual_is_long(const ResArgs& a);
+hipError_t launch_residual_long(const ResArgs& a, hipStream_t s);
+int64_t residual_long_floats(const ResArgs& a);
+hipError_t launch_residual_long_backward(const ResArgs& a, hipStream_t s);
+
 // Rows of any length (gtp_res_any.hip).
 hipError_t launch_residual_any(const ResArgs& a, hipStream_t s);
 int64_t residual_any_floats(const ResArgs& a);

@@ -188,7 +188,7 @@ bool residual_layout(const ResArgs& a, bool wide, bool back, ResLay* out) {
 hipError_t launch_residual(const ResArgs& a, hipStream_t s) {
   ResLay y;
   if (!residual_layout(a, wide16(a.x) && wide16(a.a) && wide16(a.r) && wide16(a.h), false, &y))
-    return launch_residual_any(a, s);
+    return residual_is_long(a) ? launch_residual_long(a, s) : launch_residual_any(a, s);
   const Forward f{a, y, s};
   if (!a.bf16) return a.L == 0 ? res_with_team<float, 4, true>(y, f) : res_with_team<float, 4, false>(y, f);
   if (y.V == 8) return a.L == 0 ? res_with_team<uint16_t, 8, true>(y, f) : res_with_team<uint16_t, 8, false>(y, f);
