@@ -13,7 +13,7 @@
 namespace gtp {
 namespace {
 
-constexpr int V = 4, kThreads = 1024, kSteps = 4;  // steps whose loads are in flight together
+constexpr int V = 4, kThreads = 1024, kSteps = 2;  // steps whose loads are in flight together: with four, 128 registers a lane spill
 typedef Spots<V, false> Place;
 typedef Team<0, V, false> Block;
 
