@@ -98,7 +98,7 @@ def build(verbose: bool = False, poison: bool = True) -> str:
     t0 = time.time()
     failed = []
     running = []
-    slow = ("gtp_mixq", "gtp_small", "gtp_escn.", "gtp_wbwd")  # the longest compilations first
+    slow = ("gtp_mixq", "gtp_small", "gtp_escn.", "gtp_wbwd", "gtp_attn_")  # the longest compilations first
     pending = sorted(jobs, key=lambda j: next((i for i, n in enumerate(slow) if n in j[1]), len(slow)))
     while pending or running:
         while pending and len(running) < 8:

@@ -13,6 +13,8 @@
 // unit 33 %; 8192 rows, 8 heads of 128, bf16: 911-946 us, 581-604 TFLOP/s, matrix and vector
 // unit 25 % each: two waves a SIMD cost it the tile ahead and 104 bytes a lane in scratch
 // memory (heads of 97-128 on two-wave workgroups 140, of 65-96 there 80).
+// With a bias by distance: two segments of 3500-4300 rows, 16 heads of 64 over 4, bf16 (the four rows of an atom share their
+// bucket): 608 us; 1777-2001 rows, 8 heads of 64, fp32, buckets made ahead: 272 us (each made at its score: 309).
 #pragma once
 
 #include "gtp_attn_core.hpp"
@@ -68,7 +70,6 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
   u32x4 ahead[BIAS == kBiasBytes ? RT : 1];
   if constexpr (BIAS != kNoBias) {
     lds_poison(more, POS + a.G * bias_stride(a.buckets));
-    load_bias(a, w.hk, more + POS);  // the loop's barriers stand before its use
     if constexpr (BIAS == kBias)
       px = a.k_pos[3 * jc], py = a.k_pos[3 * jc + 1], pz = a.k_pos[3 * jc + 2];
     else
@@ -107,6 +108,7 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
   int64_t r0 = w.split * per * BR;
   constexpr bool AHEAD = !long_rows<T, DP>() && !(sizeof(T) == 2 && DP == 128);  // there the registers hold no more
   if (AHEAD && r0 < r_end) fetch(r0);
+  if constexpr (BIAS != kNoBias) load_bias(a, w.hk, more + POS);  // behind the first tile's loads; the loop's barriers stand before its use
   for (; r0 < r_end; r0 += BR) {
     if (!AHEAD) fetch(r0);
     __syncthreads();
@@ -141,13 +143,13 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
       f32x16 p;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const int row = 32 * t + 8 * g + 4 * hi;
         typedef int i32x4 __attribute__((ext_vector_type(4)));
         uint32_t in = 0;
         i32x4 head_at = {0, 0, 0, 0};
+        const int row = 32 * t + 8 * g + 4 * hi;
         if constexpr (BIAS == kBias) head_at = *reinterpret_cast<const i32x4*>(t_head + row);
-        const f32x4 rf = *reinterpret_cast<const f32x4*>(t_ref + row);
-        const f32x4 de = *reinterpret_cast<const f32x4*>(t_delta + row);
+        const f32x4 rf = *reinterpret_cast<const f32x4*>(t_ref + 32 * t + 8 * g + 4 * hi);
+        const f32x4 de = *reinterpret_cast<const f32x4*>(t_delta + 32 * t + 8 * g + 4 * hi);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int r = 4 * g + i;

@@ -29,7 +29,9 @@
 // keys, products), on that two-wave form: 64 of them, 8 heads of 72, fp32: 21.4-22.8 us.
 // Heads above 128 fill the registers with one wave a SIMD, fp32 ones spill (372 bytes a lane
 // at 193-256): 4001 rows, 4 heads of 200: bf16 176 us, 291 TFLOP/s, fp32 730 us, 70.
-// With a bias by distance (BIAS, see Buckets) the vector unit has twice the work for a score.
+// With a bias by distance (see Buckets) a score takes twice the vector instructions, 20 instead of 10, or, with its
+// bucket made ahead for all heads (gtp_attn_bytes.hip), 11 and an LDS read.  8192 rows, 8 heads of 128, 32 buckets,
+// bf16: 549 us so, 447 with the buckets made ahead (their making 20 of it).  Molecules as above: 25.3 us.
 #pragma once
 
 #include "gtp_attn_core.hpp"
@@ -78,7 +80,6 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const A
   u32x4 ahead[BIAS == kBiasBytes ? KT : 1];
   if constexpr (BIAS != kNoBias) {
     lds_poison(more, POS + a.G * bias_stride(a.buckets));
-    load_bias(a, w.hk, more + POS);  // the loop's barriers stand before its use
     table = more + POS + g * bias_stride(a.buckets);
     if constexpr (BIAS == kBias)
       px = a.q_pos[3 * qi], py = a.q_pos[3 * qi + 1], pz = a.q_pos[3 * qi + 2];
@@ -118,6 +119,7 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const A
   int64_t j0 = w.split * per * BN;
   constexpr bool AHEAD = !long_rows<T, DP>();
   if (AHEAD && j0 < j_end) fetch(j0);
+  if constexpr (BIAS != kNoBias) load_bias(a, w.hk, more + POS);  // behind the first tile's loads; the loop's barriers stand before its use
   for (; j0 < j_end; j0 += BN) {
     if (!AHEAD) fetch(j0);
     __syncthreads();
@@ -210,7 +212,7 @@ __global__ __launch_bounds__(64 * NW, DP <= 128 ? 2 : 1) void k_attn_fwd(const A
   }
   l = half_sum(l);
   if (!there) return;
-  if (l == 0.0f)  // an empty row: zeros, whatever v holds (a zero times an infinity would be NaN)
+  if (BIAS != kNoBias && l == 0.0f)  // nothing within the cutoff: zeros, whatever v holds (0 times infinity would be NaN)
 #pragma unroll
     for (int i = 0; i < NDT; ++i) acc[i] = zero16();
   const float inv = l == 0.0f ? 0.0f : (DROP ? a.keep / l : 1.0f / l);

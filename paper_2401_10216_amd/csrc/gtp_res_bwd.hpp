@@ -5,6 +5,12 @@
 // weights' four sums stay in registers too, one for each place and step, over all rows that a team takes; at the
 // end the teams' are added in order and each workgroup leaves a part.  The gate's gradient sums a channel's
 // coefficients, which lie on neighbouring places, through LDS.
+//
+// Measured with the sum of the parts: fp32, 8192 x 128 channels of degree 6 325 us (3.8 TB/s; 326 the kernel), 16384 of
+// degree 3 191 us (4.3), of degree 1 54 us (4.1), 65536 x 256 scalars 118 us (4.5); 1728 x 256 of degree 2 44 us (37 and 5).
+// What bounds it is the registers: an element takes seven of 32 bits (four tensors, two sums, g1), so a SIMD holds one
+// or two waves, whose barriers, LDS reads and loads nothing else hides; vector unit 40 % busy.  In bf16 an element takes
+// as many instructions for half the bytes: 16384 x 128 of degree 3 184 us (2.2 TB/s), 50001 x 500 scalars 98 us (3.1).
 #pragma once
 
 #include <algorithm>

@@ -1,5 +1,11 @@
 // The residual step, forward, rows in registers (formulas in gtp_res.hpp, rows and teams in
 // gtp_res_row.hpp).  HBM bounds it: x, a and the gate read once, r and h written once.
+//
+// Measured (copies on this chip: 5.5 TB/s): fp32 rows of 128 channels, 16384 of degree 1 28.8 us (4.95 TB/s), of degree
+// 3 117 us (4.7), of degree 6 377 us (4.4); 64 channels of degree 8 277 us (4.9); 65536 rows of 256 scalars 69 us (4.9);
+// bf16, 32768 x 128 of degree 6, no norm behind the part: 419 us (3.9: twice as many elements a byte, some 20 vector
+// instructions each, and every second workgroup of the CU in a barrier).  1728 x 256 of degree 2: 25 us (2.6), seven rows a
+// CU, a load, two sums and a store one after the other; 27 rows: 9.7 us, of which a launch is 3 and the tables 2.
 #include <algorithm>
 
 #include "gtp_res_row.hpp"

@@ -200,6 +200,13 @@ def _want(t, name, shape, dtypes, device=None):
     return t.data_ptr()
 
 
+def _ptr_of(t, name, shape, dtype, device, plain):
+    """_want for one dtype, in half the time where nothing is wrong (plain: torch.Tensor; shape: a tuple of ints)."""
+    if (type(t) is plain and t.dtype == dtype and t.shape == shape and t.device == device and t.is_contiguous()):
+        return t.data_ptr()
+    return _want(t, name, shape, (dtype,), device)
+
+
 def _on_gpu(t, name):
     """Last check before a call: the operands (all on t's device) are device tensors."""
     if not t.is_cuda:
@@ -597,15 +604,21 @@ def _residual(x, a, L, gate, scale, w_post, b_post, w_pre, b_pre, post, eps):
     """Validated fields of gtp_residual, and the data pointers of x and a."""
     if x.dim() != 3 or x.shape[2] != nsh(L):
         raise ValueError("x must be [N, C, (L+1)^2]")
-    N, C, _ = x.shape
-    dev, one, own = x.device, _f32(), (x.dtype,)
+    import torch
+    N, C, _ = shape = x.shape
+    dev, own, f32, plain = x.device, x.dtype, torch.float32, torch.Tensor
     code = _dtype_code(x)
     if not post and (w_post is not None or b_post is not None):
         raise ValueError("w_post and b_post need post")
-    ptr = [_opt(t, name, shape, types, dev) or 0 for t, name, shape, types in (
-        (scale, "scale", (L + 1, C), one), (w_post, "w_post", (L + 1, C), one), (b_post, "b_post", (C,), one),
-        (w_pre, "w_pre", (L + 1, C), one), (b_pre, "b_pre", (C,), one), (gate, "gate", (N, C), own))]
-    return (L, code, N, C, 1 if post else 0, eps, *ptr), _want(x, "x", x.shape, own), _want(a, "a", x.shape, own, dev)
+    table, row = (L + 1, C), (C,)
+    return (L, code, N, C, 1 if post else 0, eps,
+            0 if scale is None else _ptr_of(scale, "scale", table, f32, dev, plain),
+            0 if w_post is None else _ptr_of(w_post, "w_post", table, f32, dev, plain),
+            0 if b_post is None else _ptr_of(b_post, "b_post", row, f32, dev, plain),
+            0 if w_pre is None else _ptr_of(w_pre, "w_pre", table, f32, dev, plain),
+            0 if b_pre is None else _ptr_of(b_pre, "b_pre", row, f32, dev, plain),
+            0 if gate is None else _ptr_of(gate, "gate", (N, C), own, dev, plain)), \
+        _ptr_of(x, "x", shape, own, dev, plain), _ptr_of(a, "a", shape, own, dev, plain)
 
 
 def gtp_residual_norm(x, a, L: int, gate=None, scale=None, w_post=None, b_post=None, w_pre=None, b_pre=None,
@@ -617,16 +630,18 @@ def gtp_residual_norm(x, a, L: int, gate=None, scale=None, w_post=None, b_post=N
     stats = (mean_post, rstd_post, mean_pre, rstd_pre), fp32 [N] and [N, L+1] (post's None without post), is what the
     backward reads.  r may be x."""
     import torch
-    f32 = torch.float32
+    f32, plain = torch.float32, torch.Tensor
     desc, px, pa = _residual(x, a, L, gate, scale, w_post, b_post, w_pre, b_pre, post, eps)
-    N, dev, own = x.shape[0], x.device, (x.dtype,)
+    N, dev, own = x.shape[0], x.device, x.dtype
     with _allocating(stream):
         r = torch.empty_like(x) if r is None else r
         h = torch.empty_like(x) if h is None else h
-        stats = tuple(torch.empty(shape, dtype=f32, device=dev) if post or i > 1 else None
-                      for i, shape in enumerate(((N,), (N, L + 1)) * 2))
-    pr = _want(r, "r", x.shape, own, dev)
-    ph = _want(h, "h", x.shape, own, dev)
+        one, each = (N,), (N, L + 1)
+        stats = (torch.empty(one, dtype=f32, device=dev) if post else None,
+                 torch.empty(each, dtype=f32, device=dev) if post else None,
+                 torch.empty(one, dtype=f32, device=dev), torch.empty(each, dtype=f32, device=dev))
+    pr = _ptr_of(r, "r", x.shape, own, dev, plain)
+    ph = _ptr_of(h, "h", x.shape, own, dev, plain)
     _on_gpu(x, "x")
     lib_ = lib()
     _check(lib_.gtp_residual_norm(_RESIDUAL.pack(*desc), px, pa, pr, ph,
@@ -646,8 +661,8 @@ def gtp_residual_norm_backward(r, a, L: int, stats, dh, dr=None, gate=None, scal
     import torch
     f32 = torch.float32
     desc, pr, pa = _residual(r, a, L, gate, scale, w_post, b_post, w_pre, b_pre, post, 1.0)
-    N, C, _ = r.shape
-    dev, own, one = r.device, (r.dtype,), _f32()
+    N, C, _ = shape = r.shape
+    dev, own, plain = r.device, r.dtype, torch.Tensor
     there = [n for n in _RESIDUAL_NEED if (gate is not None or n != "dgate") and (post or not n.endswith("_post"))]
     need = there if need is None else need
     unknown = set(need) - set(there)
@@ -655,10 +670,10 @@ def gtp_residual_norm_backward(r, a, L: int, stats, dh, dr=None, gate=None, scal
         raise ValueError(f"unknown gradients {sorted(unknown)}")
     if len(stats) != 4:
         raise ValueError("stats must be what gtp_residual_norm returned")
-    ps = [_want(t, name, shape, one, dev) if post or i > 1 else 0 for i, (t, name, shape) in enumerate(zip(
+    ps = [_ptr_of(t, name, size, f32, dev, plain) if post or i > 1 else 0 for i, (t, name, size) in enumerate(zip(
         stats, ("mean_post", "rstd_post", "mean_pre", "rstd_pre"), ((N,), (N, L + 1)) * 2))]
-    pdh = _want(dh, "dh", r.shape, own, dev)
-    pdr = _opt(dr, "dr", r.shape, own, dev)
+    pdh = _ptr_of(dh, "dh", shape, own, dev, plain)
+    pdr = None if dr is None else _ptr_of(dr, "dr", shape, own, dev, plain)
     _on_gpu(r, "r")
     lib_ = lib()
     d = _RESIDUAL.pack(*desc)
@@ -674,7 +689,7 @@ def gtp_residual_norm_backward(r, a, L: int, stats, dh, dr=None, gate=None, scal
                 out[n] = torch.empty((C,) if n.startswith("db") else (L + 1, C), dtype=f32, device=dev)
         work = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes > 0 else None
     if dx is not None and "dx" in out:
-        _want(dx, "dx", r.shape, own, dev)
+        _ptr_of(dx, "dx", shape, own, dev, plain)
     _check(lib_.gtp_residual_norm_backward(d, pr, pa, _RESIDUAL_STATS.pack(*ps), pdh, pdr,
                                            _RESIDUAL_GRADS.pack(*[_ptr(out.get(n)) or 0 for n in _RESIDUAL_NEED]),
                                            _ptr(work), nbytes, _stream(stream)), lib_)
@@ -841,13 +856,17 @@ def gtp_attention_bias_edges(buckets: int, r0: float, per_octave: int = 4) -> li
 def _bias(bias, q_pos, k_pos, r0, per_octave, q, k):
     """Packed gtp_attn_bias."""
     import torch
-    dev, one = q.device, _f32()
-    if not isinstance(bias, torch.Tensor) or bias.dim() != 2:
+    dev, f32, plain = q.device, torch.float32, torch.Tensor
+    if not isinstance(bias, plain) or bias.dim() != 2:
         raise ValueError("bias must be [H, buckets]")
-    pb = _want(bias, "bias", (q.shape[1], bias.shape[1]), one, dev)
-    pq = _want(q_pos, "q_pos", (q.shape[0], 3), one, dev)
-    pk = pq if k_pos is None and k.shape[0] == q.shape[0] else _want(k_pos, "k_pos", (k.shape[0], 3), one, dev)
-    return _BIAS.pack(pb, pq, pk, r0 * r0, bias.shape[1], per_octave)
+    Tq, Tk = q.shape[0], k.shape[0]
+    pb = _ptr_of(bias, "bias", (q.shape[1], bias.shape[1]), f32, dev, plain)
+    pq = _ptr_of(q_pos, "q_pos", (Tq, 3), f32, dev, plain)
+    pk = pq if k_pos is None and Tk == Tq else _ptr_of(k_pos, "k_pos", (Tk, 3), f32, dev, plain)
+    try:
+        return _BIAS.pack(pb, pq, pk, r0 * r0, bias.shape[1], per_octave)
+    except (OverflowError, struct.error) as e:  # beyond fp32, or not a whole number
+        raise ValueError(f"r0 and per_octave must be a number and a whole number within range: {e}") from None
 
 
 def gtp_attention_biased(q, k, v, bias, q_pos, k_pos=None, r0: float = 1.0, per_octave: int = 4, scale=None, q_off=None,

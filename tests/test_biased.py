@@ -101,6 +101,7 @@ CASES = [
     ([600, 433], [600, 433], 4, 4, 64, 0, 0, dict(buckets=64, per=8, box=9.0)), ([300, 511], [520, 400], 8, 4, 72, 0.2, 0.1, {}),
     ([289], [1000], 4, 1, 120, 0, 0, dict(cutoff=True)), ([700], [545], 4, 4, 32, 0.5, 0, {}), ([513], [257], 6, 2, 190, 0, 0.1, {}),
     ([300], [300], 4, 4, 250, 0.1, 0, dict(buckets=64)), ([401, 0, 399], [0, 300, 390], 4, 4, 96, 0, 0, {}),
+    ([3], [40], 63, 1, 190, 0, 0, dict(buckets=64)), ([5], [33], 256, 1, 9, 0, 0, dict(buckets=16)),
     ([20], [500], 64, 1, 16, 0, 0, dict(buckets=64)), ([9], [40], 37, 1, 20, 0, 0.2, dict(buckets=5)),
 ]
 

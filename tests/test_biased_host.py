@@ -137,6 +137,7 @@ def test_binding_refusals():
             (lambda: b(q, k, k, bias, pos, kpos, 1.0, 4, q, q, lse, need=("dpos",)), ValueError),
             (lambda: b(q, k, k, bias, pos, kpos, 1.0, 4, q, q, z(6, 3)), ValueError),
             (lambda: b(q, k, k, bias, pos, kpos, 1.0, 4, q, z(6, 4, 7), lse), ValueError),
+            (lambda: f(q, k, k, bias, pos, kpos, 1e30), ValueError), (lambda: f(q, k, k, bias, pos, kpos, 1.0, 2.5), ValueError),
             (lambda: b(q, k, k, bias, pos, kpos, 1.0, 4, q, q, lse), ValueError)):  # not device tensors
         with pytest.raises(error):
             call()
