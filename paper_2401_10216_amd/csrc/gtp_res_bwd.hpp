@@ -10,7 +10,7 @@
 // degree 3 191 us (4.3), of degree 1 54 us (4.1), 65536 x 256 scalars 118 us (4.5); 1728 x 256 of degree 2 44 us (37 and 5).
 // What bounds it is the registers: an element takes seven of 32 bits (four tensors, two sums, g1), so a SIMD holds one
 // or two waves, whose barriers, LDS reads and loads nothing else hides; vector unit 40 % busy.  In bf16 an element takes
-// as many instructions for half the bytes: 16384 x 128 of degree 3 184 us (2.2 TB/s), 50001 x 500 scalars 98 us (3.1).
+// as many instructions for half the bytes: 16384 x 128 of degree 3 184 us (2.2 TB/s), 50001 x 500 scalars 86 us (3.5).
 #pragma once
 
 #include <algorithm>
@@ -275,10 +275,12 @@ __global__ __launch_bounds__(MAXT) void k_res_backward(const ResArgs a, const Re
 }
 
 // Workgroups: as many as the CUs hold at once (each makes the tables and leaves a part of the weights' gradients), and
-// two rows a team at least, where that fills the chip.
+// two rows a team at least, where that fills the chip.  50001 rows of 500 scalars, bf16, 2 steps of a wave: 512 workgroups
+// 100 us, 768 86, 1024 110.
 inline int64_t res_grid(int64_t N, const ResLay& y) {
   const int64_t rows = (N + y.teams() - 1) / y.teams();
-  const int64_t n = std::min<int64_t>(rows, y.threads > kTeamThreads || y.NI > 4 ? 256 : 512), half = (rows + 1) / 2;
+  const int64_t n = std::min<int64_t>(rows, y.threads > kTeamThreads || y.NI > 4 ? 256 : y.NI > 2 ? 512 : 768),
+                half = (rows + 1) / 2;
   return n <= half ? n : std::max<int64_t>(half, std::min<int64_t>(n, 256));
 }
 
