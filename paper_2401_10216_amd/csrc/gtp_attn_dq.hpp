@@ -72,9 +72,9 @@ __global__ __launch_bounds__(64 * NW, (waves_per_simd<T, DP>())) void k_attn_dq(
   qf.load(static_cast<const T*>(a.q.p) + qi * a.q.row + h * a.q.head, there, hi, a.d, a.vec);
   gf.load(static_cast<const T*>(a.dout.p) + qi * a.dout.row + h * a.dout.head, there, hi, a.d, a.vec);
   // The matrix unit's sums are cut downwards, some 2^-27 of a value's size on average, which a
-  // bucket's sum of a million dS of both signs would show: every other wave has dout with
-  // its sign turned.
-  const float turn = BIAS && ((wave ^ w.tile ^ int(w.b)) & 1) ? -1.0f : 1.0f;
+  // bucket's sum of many dS of both signs would show: every other wave, and every other part of
+  // the keys, has dout with its sign turned.
+  const float turn = BIAS && ((wave ^ w.tile ^ w.split ^ int(w.b)) & 1) ? -1.0f : 1.0f;
   if (BIAS && turn < 0.0f) gf.negate();
   // rows without a key, and rows past the end: every exponential is zero
   const float lse = there ? a.lse[qi * a.H + h] : -INFINITY;
