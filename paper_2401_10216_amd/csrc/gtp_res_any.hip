@@ -194,13 +194,18 @@ __global__ __launch_bounds__(kThreads) void k_res_gradients(const Back<T> b, T* 
     const int64_t base = n * C * K;
     const float* const m = b.means + n * 2 * (L + 2) + L + 2;
     if (dgate) {
-      for (int64_t c = threadIdx.x; c < C; c += kThreads) {
+      // a channel to a thread, or, of degree 3 and more, to a wave
+      const int lanes = K < 16 ? 1 : 64, lane = threadIdx.x & (lanes - 1);
+      for (int64_t c = threadIdx.x / lanes; c < C; c += kThreads / lanes) {
         float s = 0.0f;
-        for (int l = 0; l <= L; ++l)
-          for (int64_t i = base + c * K + l * l; i < base + c * K + (l + 1) * (l + 1); ++i) {
-            const float t = b.w.post ? fmaf(b.xh1(n, l, i), b.w.post_w(l, c), b.w.post_b(l, c)) : ld(b.a, i);
-            s = fmaf(b.d(n, l, c, i) * b.w.s(l, c), t, s);
-          }
+        for (int k = lane; k < int(K); k += lanes) {
+          const int l = degree_of(k);
+          const int64_t i = base + c * K + k;
+          const float t = b.w.post ? fmaf(b.xh1(n, l, i), b.w.post_w(l, c), b.w.post_b(l, c)) : ld(b.a, i);
+          s = fmaf(b.d(n, l, c, i) * b.w.s(l, c), t, s);
+        }
+        if (lanes == 64) s = wave_sum(s);
+        if (lane != 0) continue;
         const float v = ld(b.gate, n * C + c);
         st(dgate, n * C + c, sigmoid(v) * sigmoid(-v) * s);
       }
@@ -222,7 +227,7 @@ __global__ __launch_bounds__(kThreads) void k_res_gradients(const Back<T> b, T* 
   }
 }
 
-// The weights' sums over a chunk of rows: workgroup (channels, chunk).
+// The weights' sums over a chunk of rows: workgroup (degree and channel, chunk).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_res_weights(const Back<T> b, int64_t chunk, float* __restrict__ partial) {
   __shared__ float red[kThreads / 64];
@@ -231,32 +236,56 @@ __global__ __launch_bounds__(kThreads) void k_res_weights(const Back<T> b, int64
   const int64_t C = b.w.C, K = int64_t(L + 1) * (L + 1), n0 = int64_t(blockIdx.y) * chunk;
   const int64_t rows = n0 + chunk < b.N ? chunk : b.N - n0;
   float* const out = partial + int64_t(blockIdx.y) * res_columns(L, C);
-  for (int64_t c = blockIdx.x; c < C; c += gridDim.x)
-    for (int l = 0; l <= L; ++l) {
-      const int64_t M = 2 * l + 1;
-      float e1 = 0.0f, e2 = 0.0f, f = 0.0f, g = 0.0f;
-      const Divide by{uint32_t(M)};
-      for (int64_t q = threadIdx.x; q < rows * M; q += kThreads) {
-        const int64_t k = q < (int64_t(1) << 31) ? by(uint32_t(q)) : q / M;
-        const int64_t n = n0 + k, i = (n * C + c) * K + l * l + (q - k * M);
-        const float u = b.d(n, l, c, i) * b.open(n, c), d = ld(b.dh, i);
-        e1 = fmaf(u, b.xh1(n, l, i), e1);
-        e2 = fmaf(d, b.xh2(n, l, i), e2);
-        f += u;
-        g += d;
-      }
-      e1 = block_sum(e1, red);
-      e2 = block_sum(e2, red);
-      if (l == 0) {
-        f = block_sum(f, red);
-        g = block_sum(g, red);
-      }
-      if (threadIdx.x == 0) {
-        out[l * C + c] = e1;
-        out[(L + 1 + l) * C + c] = e2;
-        if (l == 0) out[2 * (L + 1) * C + c] = f, out[(2 * L + 3) * C + c] = g;
-      }
+  for (int64_t id = blockIdx.x; id < C * (L + 1); id += gridDim.x) {
+    const int l = int(id / C);
+    const int64_t c = id - l * C, M = 2 * l + 1;
+    float e1 = 0.0f, e2 = 0.0f, f = 0.0f, g = 0.0f;
+    const Divide by{uint32_t(M)};
+    for (int64_t q = threadIdx.x; q < rows * M; q += kThreads) {
+      const int64_t k = q < (int64_t(1) << 31) ? by(uint32_t(q)) : q / M;
+      const int64_t n = n0 + k, i = (n * C + c) * K + l * l + (q - k * M);
+      const float u = b.d(n, l, c, i) * b.open(n, c), d = ld(b.dh, i);
+      e1 = fmaf(u, b.xh1(n, l, i), e1);
+      e2 = fmaf(d, b.xh2(n, l, i), e2);
+      f += u;
+      g += d;
     }
+    e1 = block_sum(e1, red);
+    e2 = block_sum(e2, red);
+    if (l == 0) {
+      f = block_sum(f, red);
+      g = block_sum(g, red);
+    }
+    if (threadIdx.x == 0) {
+      out[l * C + c] = e1;
+      out[(L + 1 + l) * C + c] = e2;
+      if (l == 0) out[2 * (L + 1) * C + c] = f, out[(2 * L + 3) * C + c] = g;
+    }
+  }
+}
+
+// The same of scalars (K = 1), a thread a channel: the other way, neighbours read a row apart.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_res_weights_scalars(const Back<T> b, int64_t chunk,
+                                                                  float* __restrict__ partial) {
+  const int64_t C = b.w.C, n0 = int64_t(blockIdx.y) * chunk, n1 = n0 + chunk < b.N ? n0 + chunk : b.N;
+  float* const out = partial + int64_t(blockIdx.y) * res_columns(0, C);
+  for (int64_t c = int64_t(blockIdx.x) * kThreads + threadIdx.x; c < C; c += int64_t(gridDim.x) * kThreads) {
+    float e1 = 0.0f, e2 = 0.0f, f = 0.0f, g = 0.0f;
+#pragma unroll 4
+    for (int64_t n = n0; n < n1; ++n) {
+      const int64_t i = n * C + c;
+      const float u = b.d(n, 0, c, i) * b.open(n, c), d = ld(b.dh, i);
+      e1 = fmaf(u, b.xh1(n, 0, i), e1);
+      e2 = fmaf(d, b.xh2(n, 0, i), e2);
+      f += u;
+      g += d;
+    }
+    out[c] = e1;
+    out[C + c] = e2;
+    out[2 * C + c] = f;
+    out[3 * C + c] = g;
+  }
 }
 
 // The parts' sums, added in order: a workgroup takes 8 columns (l, c) of E1 and E2 at a time
@@ -331,8 +360,13 @@ hipError_t run_any_backward(const ResArgs& a, hipStream_t s) {
                   a.rstd2, a.work, a.N, a.L};
   const uint32_t grid = uint32_t(std::min(a.N, kGrid));
   k_res_means<T><<<grid, kThreads, 0, s>>>(b);
-  if (a.weights())  // before dx, which may be written over dr
-    k_res_weights<T><<<dim3{uint32_t(std::min(a.C, kGrid)), uint32_t(used)}, kThreads, 0, s>>>(b, chunk, a.work + means);
+  // the weights before dx, which may be written over dr
+  if (a.weights() && a.L == 0 && a.C >= kThreads)
+    k_res_weights_scalars<T><<<dim3{uint32_t(std::min((a.C + kThreads - 1) / kThreads, kGrid / used)), uint32_t(used)},
+                               kThreads, 0, s>>>(b, chunk, a.work + means);
+  else if (a.weights())
+    k_res_weights<T><<<dim3{uint32_t(std::min(a.C * (a.L + 1), kGrid / used)), uint32_t(used)}, kThreads, 0, s>>>(
+        b, chunk, a.work + means);
   if (a.dx || a.da || a.dgate)
     k_res_gradients<T><<<grid, kThreads, 0, s>>>(b, static_cast<T*>(a.dx), static_cast<T*>(a.da),
                                                  static_cast<T*>(a.dgate));

@@ -600,10 +600,10 @@ def gtp_layer_norm_backward(x, dy, L: int, mean, rstd, w=None, need=("dx", "dw",
     return out
 
 
-def _residual(x, a, L, gate, scale, w_post, b_post, w_pre, b_pre, post, eps):
-    """Validated fields of gtp_residual, and the data pointers of x and a."""
+def _residual(x, a, L, gate, scale, w_post, b_post, w_pre, b_pre, post, eps, name="x"):
+    """Validated fields of gtp_residual, and the data pointers of x (called `name`) and a."""
     if x.dim() != 3 or x.shape[2] != nsh(L):
-        raise ValueError("x must be [N, C, (L+1)^2]")
+        raise ValueError(f"{name} must be [N, C, (L+1)^2]")
     import torch
     N, C, _ = shape = x.shape
     dev, own, f32, plain = x.device, x.dtype, torch.float32, torch.Tensor
@@ -618,7 +618,7 @@ def _residual(x, a, L, gate, scale, w_post, b_post, w_pre, b_pre, post, eps):
             0 if w_pre is None else _ptr_of(w_pre, "w_pre", table, f32, dev, plain),
             0 if b_pre is None else _ptr_of(b_pre, "b_pre", row, f32, dev, plain),
             0 if gate is None else _ptr_of(gate, "gate", (N, C), own, dev, plain)), \
-        _ptr_of(x, "x", shape, own, dev, plain), _ptr_of(a, "a", shape, own, dev, plain)
+        _ptr_of(x, name, shape, own, dev, plain), _ptr_of(a, "a", shape, own, dev, plain)
 
 
 def gtp_residual_norm(x, a, L: int, gate=None, scale=None, w_post=None, b_post=None, w_pre=None, b_pre=None,
@@ -660,7 +660,7 @@ def gtp_residual_norm_backward(r, a, L: int, stats, dh, dr=None, gate=None, scal
     write to, which may be dr."""
     import torch
     f32 = torch.float32
-    desc, pr, pa = _residual(r, a, L, gate, scale, w_post, b_post, w_pre, b_pre, post, 1.0)
+    desc, pr, pa = _residual(r, a, L, gate, scale, w_post, b_post, w_pre, b_pre, post, 1.0, "r")
     N, C, _ = shape = r.shape
     dev, own, plain = r.device, r.dtype, torch.Tensor
     there = [n for n in _RESIDUAL_NEED if (gate is not None or n != "dgate") and (post or not n.endswith("_post"))]

@@ -110,7 +110,7 @@ class Case:
 SHAPES = [(1, 1, 0), (3, 1, 0), (5, 7, 0), (33, 256, 0), (3, 300, 0), (2, 5000, 0), (1, 70001, 0), (700, 17, 0), (4097, 20, 0),
           (65, 500, 0), (1, 1, 1), (7, 5, 1), (1000, 16, 1), (33, 16, 2), (27, 128, 2), (257, 64, 2), (300, 256, 2), (3, 1000, 3),
           (40, 33, 4), (9, 128, 6), (130, 30, 6), (4, 64, 8), (7, 300, 8), (3, 65, 12), (3, 64, 16), (2, 3, 20), (2, 2, 64),
-          (1, 600, 8)]
+          (1, 600, 8), (130, 5003, 0)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
