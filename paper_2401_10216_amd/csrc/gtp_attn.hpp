@@ -49,7 +49,10 @@ __host__ __device__ inline int64_t bytes_tiles(int64_t most) { return (most + 63
 constexpr int kMaxBias = 4096, kMaxBiasHeads = 256;  // of the bias of a key head's query heads, in LDS
 // From one head's to the next: odd, so that heads that share a distance (lanes side by side) read different banks.
 __host__ __device__ inline int bias_stride(int buckets) { return buckets | 1; }
-int dq_rows_a_tile(const AttnArgs& a);  // of dq: a bias's sums beside the longest fp32 tiles fit the LDS of 64 rows only
+// Of dq.  A bias's sums beside the longest fp32 tiles fit the LDS of 64 rows only; where two workgroups of 128 rows do not
+// fit a CU's and one of 256 does, that keeps two waves on a SIMD (two of 3500-4300 rows, 8 heads of 128, 64 buckets, bf16:
+// 540 us, of 128 rows 770).
+int dq_rows_a_tile(const AttnArgs& a);
 int attn_padded(int d);  // the head length that the kernels are instantiated at, >= d
 // Parts that the keys of each row (the rows of each key) are dealt to: 1 where the
 // workgroups fill the chip without.

@@ -23,16 +23,18 @@ namespace gtp {
 namespace {
 
 // Keys, values and both accumulators take twice what dq's rows do.
-template <typename T, int DP>
+// With a bias, 16-bit heads of 97-128 on one wave with the tile ahead: two of 3500-4300 rows, 8 heads of 128, buckets made
+// ahead, 859 us (two waves: 973), over 2, made at each score, 908 (1050); heads of 96, 8 over 2: 800 so, 715 on two.
+template <typename T, int DP, int BIAS>
 constexpr int dkv_waves() {
-  return DP * int(sizeof(T)) <= 128 || (sizeof(T) == 2 && DP <= 128) ? 2 : 1;
+  return DP * int(sizeof(T)) <= 128 || (sizeof(T) == 2 && DP <= (BIAS ? 96 : 128)) ? 2 : 1;
 }
 
 // Workgroup: 32 NW keys of one key head (a wave 32), rows in tiles of 32.  Heads
 // longer than 128 are dealt to `parts` workgroups by output elements (DO each):
 // the accumulators of all of them would not fit the registers.
 template <typename T, int DP, int DO, int RT, bool DROP, int BIAS, int NW>
-__global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(const AttnArgs a, int64_t n_wg, int tiles) {
+__global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP, BIAS>())) void k_attn_dkv(const AttnArgs a, int64_t n_wg, int tiles) {
   constexpr int NT = 64 * NW, BK = 32 * NW, BR = 32 * RT, NC = DP / 16, NDT = DO / 32, PARTS = DP / DO;
   __shared__ __align__(16) char tq[tile_bytes<T, DP, BR>()];
   __shared__ __align__(16) char tg[tile_bytes<T, DP, BR>()];
@@ -106,7 +108,7 @@ __global__ __launch_bounds__(64 * NW, (dkv_waves<T, DP>())) void k_attn_dkv(cons
       for (int t = 0; t < RT; ++t) ahead[t] = bytes[((r0 >> 5) + t) * 64];
   };
   int64_t r0 = w.split * per * BR;
-  constexpr bool AHEAD = !long_rows<T, DP>() && !(sizeof(T) == 2 && DP == 128);  // there the registers hold no more
+  constexpr bool AHEAD = !long_rows<T, DP>() && !(sizeof(T) == 2 && DP == 128 && BIAS == kNoBias);  // there the registers hold no more
   if (AHEAD && r0 < r_end) fetch(r0);
   if constexpr (BIAS != kNoBias) load_bias(a, w.hk, more + POS);  // behind the first tile's loads; the loop's barriers stand before its use
   for (; r0 < r_end; r0 += BR) {

@@ -247,6 +247,11 @@ template <typename T, int DP, bool DROP, int BIAS>
 void launch_tiles(const AttnArgs& a, hipStream_t s) {
   const int64_t BM = dq_rows_a_tile(a), tiles = (a.max_q * a.G + BM - 1) / BM, n = tiles * a.splits * a.Hk * a.B;
   const size_t lds = BIAS ? ((BIAS == kBias ? 3 * 32 : 0) + size_t(a.G) * bias_stride(a.buckets) + (a.dbias ? size_t(a.buckets) * 2 * BM : 0)) * 4 : 0;
+  if constexpr (BIAS != kNoBias && waves_per_simd<T, DP>() == 2)
+    if (BM == 256) {
+      k_attn_dq<T, DP, DROP, BIAS, 8><<<uint32_t(n), 512, lds, s>>>(a, n, int(tiles));
+      return;
+    }
   if constexpr (BIAS == kBiasBytes)  // made for long segments only
     k_attn_dq<T, DP, DROP, BIAS, 4><<<uint32_t(n), 256, lds, s>>>(a, n, int(tiles));
   else if (BM == 64)

@@ -138,7 +138,16 @@ int parts_for(int64_t n, int64_t length, int step, int per_cu, bool bf16) {
 int attn_padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256; }
 
 int dq_rows_a_tile(const AttnArgs& a) {
-  return a.bias && !a.bf16 && attn_padded(a.d) > 192 ? 64 : rows_a_tile(a.max_q * a.G);
+  const int DP = attn_padded(a.d), parts = a.bf16 ? 1 : 3;
+  const int64_t rows = a.max_q * a.G;
+  if (!a.bias) return rows_a_tile(rows);
+  if (!a.bf16 && DP > 192) return 64;
+  // LDS: two tiles of 32 rows, positions, the bias, a column of sums a lane
+  auto lds = [&](int64_t lanes) {
+    return 2 * 32 * parts * (2 * DP + 16) + 384 + (a.G * bias_stride(a.buckets) + lanes * a.buckets) * 4;
+  };
+  const int64_t all = 160 << 10;
+  return rows >= 512 && DP * (a.bf16 ? 2 : 4) <= 256 && lds(256) > all / 2 && lds(512) <= all ? 256 : rows_a_tile(rows);
 }
 
 // Workgroups that a CU holds: by the waves a SIMD that the kernels' registers are cut for.
@@ -151,7 +160,7 @@ int attn_row_splits(const AttnArgs& a, bool backward) {
 int attn_key_splits(const AttnArgs& a) {
   const int BK = rows_a_tile(a.max_k), DP = attn_padded(a.d), bytes = DP * (a.bf16 ? 2 : 4);
   return parts_for((a.max_k + BK - 1) / BK * (DP > 128 ? 2 : 1) * a.Hk * a.B, a.max_q * a.G, bytes <= 128 ? 64 : 32,
-                   (bytes <= (a.bf16 ? 256 : 128) ? 2 : 1) * 128 / BK, a.bf16);
+                   (bytes <= (a.bf16 ? a.bias ? 192 : 256 : 128) ? 2 : 1) * 128 / BK, a.bf16);
 }
 
 hipError_t launch_attn_sum(const AttnArgs& a, const float* part, int splits, bool keys, const AttnRows& out,

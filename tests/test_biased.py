@@ -101,6 +101,10 @@ CASES = [
     ([600, 433], [600, 433], 4, 4, 64, 0, 0, dict(buckets=64, per=8, box=9.0)), ([300, 511], [520, 400], 8, 4, 72, 0.2, 0.1, {}),
     ([289], [1000], 4, 1, 120, 0, 0, dict(cutoff=True)), ([700], [545], 4, 4, 32, 0.5, 0, {}), ([513], [257], 6, 2, 190, 0, 0.1, {}),
     ([300], [300], 4, 4, 250, 0.1, 0, dict(buckets=64)), ([401, 0, 399], [0, 300, 390], 4, 4, 96, 0, 0, {}),
+    # workgroups of eight waves, for two on a SIMD beside the sums
+    ([520, 37, 260], [300, 290, 5], 4, 4, 128, 0.2, 0.1, dict(buckets=64)), ([300, 150], [270, 80], 8, 2, 100, 0, 0.1, dict(buckets=64)),
+    ([1100], [70], 2, 1, 128, 0, 0, dict(buckets=64)), ([70, 33], [60, 20], 16, 1, 96, 0.1, 0, dict(buckets=64)),
+    ([513], [700], 4, 2, 60, 0, 0, dict(buckets=64, cutoff=True)),
     ([3], [40], 63, 1, 190, 0, 0, dict(buckets=64)), ([5], [33], 256, 1, 9, 0, 0, dict(buckets=16)),
     ([20], [500], 64, 1, 16, 0, 0, dict(buckets=64)), ([9], [40], 37, 1, 20, 0, 0.2, dict(buckets=5)),
 ]
