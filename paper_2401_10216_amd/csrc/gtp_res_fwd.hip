@@ -137,7 +137,8 @@ struct Forward {
   hipError_t operator()() const {
     const int64_t K = int64_t(a.L + 1) * (a.L + 1), teams = y.teams(), rows = (a.N + teams - 1) / teams;
     const size_t lds = size_t(res_lds(y, K, a.L, false));
-    // workgroups that the CUs hold at once, by the registers that a row's elements take: each makes the tables
+    // workgroups that the CUs hold at once, by the registers that a row's elements take: each makes the tables (12927 x 21
+    // of degree 8, fp32: four 99 us, six 115)
     const int64_t held = std::clamp<int64_t>(12 / std::max(1, NI * V * int(sizeof(T)) / 16), 1, 4);
     const int64_t fill = 256 * std::max<int64_t>(1, held * kTeamThreads / y.threads);
     k_res<T, V, NI, W, K1><<<uint32_t(std::min(rows, fill)), y.threads, lds, s>>>(a, ResWeights(a), y.A);
