@@ -489,7 +489,11 @@ gtp_status gtp_attention_bias_edges(float r0sq, int buckets, int per_octave, flo
 
 /* gtp_attention with a bias: s = scale q k^T + bias[h, bucket] (b: not NULL; the bias's values are
  * multiplied by log2(e), within fp32's range).  GTP_ERR_UNSUPPORTED where a key head has more than 256
- * query heads, or they have more than 4096 biases in all.  Else as gtp_attention. */
+ * query heads, or they have more than 4096 biases in all.  Else as gtp_attention.
+ * `work` of both directions, whichever gradients are asked for, may hold the buckets of all pairs
+ * besides, a byte each for all heads: from 4 heads and segments of more than 256 rows and keys on, and
+ * 1 GiB at most, B ceil64(max_q) ceil64(max_k) bytes (ceil64: rounded up to a multiple of 64); where they would
+ * be more, each score makes its own, and nothing of size rows x keys is stored. */
 int64_t gtp_attention_biased_work(const gtp_attn *a, const gtp_attn_bias *b, int backward);
 gtp_status gtp_attention_biased(const gtp_attn *a, const gtp_attn_bias *b, const gtp_rows *q, const gtp_rows *k,
                                 const gtp_rows *v, const gtp_rows *o, float *lse, void *work, int64_t work_bytes,
@@ -497,7 +501,8 @@ gtp_status gtp_attention_biased(const gtp_attn *a, const gtp_attn_bias *b, const
 
 /* Its gradient: dq, dk, dv as gtp_attention_backward, and
  *   dbias[h, c] = sum of dS over the pairs of bucket c   [H, buckets] fp32, or NULL,
- * written, not accumulated, summed in a fixed order.  Positions have no gradient: the bias is piecewise constant. */
+ * written, not accumulated, summed in a fixed order (`work` has a table [H / Hk, buckets] for each 64 to 256 rows of a key
+ * head and segment besides).  Positions have no gradient: the bias is piecewise constant. */
 gtp_status gtp_attention_biased_backward(const gtp_attn *a, const gtp_attn_bias *b, const gtp_rows *q,
                                          const gtp_rows *k, const gtp_rows *v, const gtp_rows *o, const gtp_rows *dout,
                                          const float *lse, const gtp_rows *dq, const gtp_rows *dk, const gtp_rows *dv,

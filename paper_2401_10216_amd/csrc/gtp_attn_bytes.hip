@@ -55,12 +55,17 @@ __global__ __launch_bounds__(256) void k_bias_bytes(const AttnArgs a, const floa
 }  // namespace
 
 // Made ahead where four heads at least share them, for segments longer than the kernels' short forms take, where their
-// making is small beside the heads' work, and where segments are not so uneven that most pairs would be of none.
+// making is small beside the heads' work, where segments are not so uneven that most pairs would be of none, and up to
+// 1 GiB, a fraction of a percent of the card's memory: what they save does not fall off with the size, but what they
+// take grows with its square, and beyond a call runs without.  8 heads of 128, bf16, forward and gradients: 32768 rows (1 GiB)
+// 7.2 and 30.2 ms (each made at its score 8.6 and 41.3), 16384 rows 1.8 and 7.6 (2.2 and 10.2); of 64, fp32, 32768 rows 14.3 and
+// 48.8 (15.6 and 62); what the limit costs: 50000 rows of 128, bf16, 20.2 and 99.8 ms instead of 17.5 and 72.8.
+constexpr int64_t kMostBytes = int64_t(1) << 30;
 int64_t bias_bytes(const AttnArgs& a) {
   if (!a.bias || a.H < 4 || a.max_q <= 256 || a.max_k <= 256 || dq_rows_a_tile(a) == 64) return 0;
   const int64_t n = a.B * bytes_tiles(a.max_q) * bytes_tiles(a.max_k);  // KB
   const double pairs = double(a.Tq) * double(a.max_k);
-  return n < (int64_t(1) << 24) && double(n) * 1024.0 <= 2.0 * pairs + 65536.0 ? n * 1024 : 0;
+  return n <= kMostBytes / 1024 && double(n) * 1024.0 <= 2.0 * pairs + 65536.0 ? n * 1024 : 0;
 }
 
 bool bias_bytes_for_keys(const AttnArgs& a) { return a.G == 1; }

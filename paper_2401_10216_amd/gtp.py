@@ -875,7 +875,9 @@ def gtp_attention_biased(q, k, v, bias, q_pos, k_pos=None, r0: float = 1.0, per_
     """gtp_attention with a learned bias[H, buckets] (fp32, up to 64 buckets) added to the scores by the distance of
     q_pos[Tq, 3] and k_pos[Tk, 3] (fp32; left out: q_pos): bucket 0 below r0, then per_octave (1, 2, 4, 8 or 16) buckets
     for each doubling of the squared distance, the last one open (gtp_attention_bias_edges names the edges).  -inf gives
-    a bucket's pairs probability zero.  Everything else, and what it returns, as gtp_attention."""
+    a bucket's pairs probability zero.  From 4 heads and segments of more than 256 rows on the call takes a byte for each pair
+    of a segment's rows and keys, up to 1 GiB (beyond, none), while it runs; so does its gradient.  Everything else, and
+    what it returns, as gtp_attention."""
     import torch
     desc, rows = _attn(q, k, v, scale, q_off, k_off, max_q, max_k, key_mask, p, rng)
     b = _bias(bias, q_pos, k_pos, r0, per_octave, q, k)

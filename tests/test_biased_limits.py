@@ -1,0 +1,65 @@
+"""Limits of the attention with a bias by distance: the work of large segments and arguments out of range (on the CPU);
+segments whose buckets are no longer made ahead (-m gpu)."""
+import ctypes
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import biased_ref as B  # noqa: E402
+from paper_2401_10216_amd import gtp  # noqa: E402
+from test_biased_host import bias_desc  # noqa: E402
+from test_layers_host import attn_desc  # noqa: E402
+
+
+def test_work_stays_bounded_for_large_segments():
+    """The buckets made ahead take a byte a pair up to 1 GiB; beyond, the work grows with the rows as without a bias."""
+    lib, GiB = gtp.lib(), 1 << 30
+    for n, B, H, Hk in ((16384, 1, 8, 8), (32768, 1, 8, 8), (32768, 1, 8, 2), (8192, 16, 4, 4), (32769, 1, 8, 8), (65536, 1, 8, 8),
+                        (131000, 1, 16, 4), (8192, 17, 4, 4), (1 << 20, 1, 4, 1)):
+        a = attn_desc(H=H, Hk=Hk, B=B, Tq=B * n, Tk=B * n, max_q=n, max_k=n)
+        pairs = B * (-(-n // 64) * 64) ** 2
+        ahead = pairs if pairs <= GiB else 0
+        more = lib.gtp_attention_biased_work(ctypes.byref(a), bias_desc(), 0) - lib.gtp_attention_work(ctypes.byref(a), 0)
+        assert more == ahead
+        # the gradient: the workgroups' tables besides, of 64 rows of a key head at least for each of 128 parts of the keys at
+        # most, and those of their sums
+        most = 128 * B * -(-n * (H // Hk) // 64) * H * 32 * 4
+        more = lib.gtp_attention_biased_work(ctypes.byref(a), bias_desc(), 1) - lib.gtp_attention_work(ctypes.byref(a), 1)
+        assert ahead <= more <= ahead + 2 * most
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [32760, 32769])  # the buckets made ahead just below 1 GiB, and at each score
+def test_rows_on_both_sides_of_the_limit(n, dtype):
+    """Some rows' results and gradients against the 64-bit form of these rows.  A lane adds up to n / 2 terms in sequence:
+    (n / 2 + 256) u of their magnitudes, and a score's error moves P by as much; bf16: 2^-8 of P and dS besides."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    H, d, nb = 4, 16, 24
+    q, k, v, do = (torch.randn((n, H, d), generator=g, device="cuda").to(dtype) for _ in range(4))
+    pos = torch.rand((n, 3), generator=g, device="cuda") * 60.0
+    bias = torch.randn((H, nb), generator=g, device="cuda")
+    print(f"biased n={n} {dtype}", flush=True)
+    o, lse = gtp.gtp_attention_biased(q, k, v, bias, pos, r0=2.0)
+    grads = gtp.gtp_attention_biased_backward(q, k, v, bias, pos, None, 2.0, 4, o, do, lse)
+    at = torch.cat([torch.arange(24, device="cuda"), torch.randint(n, (24,), generator=g, device="cuda"),
+                    torch.arange(n - 24, n, device="cuda")])
+    m = len(at)
+    args = (q[at].double(), k.double(), v.double(), bias.double(), pos[at], pos, 4.0, 4, 1.0 / math.sqrt(d), [(0, m)], [(0, n)],
+            None, 0.0, None, m, n)
+    largest = 1 + float(q.double().norm(dim=-1).amax() * k.double().norm(dim=-1).amax()) / math.sqrt(d) + float(bias.abs().max())
+    c, half = (n / 2 + 256) * 2.0 ** -24 * largest, 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -23
+    want, wl, size = B.attention(*args)
+    assert bool(((o[at].double() - want).abs() <= half * want.abs() + (half + c) * size).all())
+    assert bool(((lse[at].double() - wl).abs() <= c).all())
+    dq, s, e32 = B.attention(*args, grad=(do[at].double(), o[at].double(), lse[at].double()))["dq"]
+    assert bool(((grads["dq"][at].double() - dq).abs() <= half * dq.abs() + half * s + c * e32).all())
+    # the gradients of keys and bias: sums over all rows, the same on both sides of the limit but for rounding; here
+    # against their sum rules: dS sums to zero over a row's keys, so dbias does over the buckets; P to one: dv to do
+    total = lambda t: t.double().sum((0, 2))  # noqa: E731
+    size = do.double().abs().sum((0, 2))
+    assert bool(((total(grads["dv"]) - total(do)).abs() <= (c + 2 * half) * size).all())
+    rows = (do.double().abs().sum(-1) * v.double().abs().amax((0, 2))).sum(0) * 2  # of |dS| by head
+    assert bool((grads["dbias"].double().sum(1).abs() <= c * rows + half * (do.double() * o.double()).abs().sum((0, 2))).all())
