@@ -89,15 +89,17 @@ __global__ __launch_bounds__(MAXT) void k_res_backward(const ResArgs a, const Re
     const bool mine = n0 + team < a.N;
     const int64_t n = n0 + team;
     const int end = pl.on ? R : 0;
+    if (W && !mine) {  // zeros instead of the last row, loaded again: it adds nothing to the weights' sums, infinite or not
+      rv.clear(), dv.clear(), qv.clear(), av.clear();
+      mu2 = mu1 = 0.0f;
+#pragma unroll
+      for (int j = 0; j < V; ++j) r2[j] = r1[j] = 0.0f;
+    }
     rv.fix(t, AV, end);
     dv.fix(t, AV, end);
     float off2[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      off2[j] = pl.zero(j, mu2);
-      r2[j] = mine ? r2[j] : 0.0f;  // a team without a row of its own adds nothing to the weights' sums: xh = 0
-    }
-    const float one = mine ? 1.0f : 0.0f;
+    for (int j = 0; j < V; ++j) off2[j] = pl.zero(j, mu2);
     if (!K1 && gate) {
       // the row before's may still be read by others of a workgroup; the ones of the row before that, behind
       // barriers, not
@@ -128,9 +130,9 @@ __global__ __launch_bounds__(MAXT) void k_res_backward(const ResArgs a, const Re
           e2[i][j] = fmaf(d[j], x, e2[i][j]);
           rv.set(i, j, x);
           dv.set(i, j, g);
-          if constexpr (K1) g0[i][j] = fmaf(d[j], one, g0[i][j]);
+          if constexpr (K1) g0[i][j] += d[j];
         }
-        if constexpr (!K1) g0[i][0] = fmaf(pl.sum_zero(d), one, g0[i][0]);
+        if constexpr (!K1) g0[i][0] += pl.sum_zero(d);
       }
     }
     float m2[V], mg2, m1[V], mg1;
@@ -177,7 +179,7 @@ __global__ __launch_bounds__(MAXT) void k_res_backward(const ResArgs a, const Re
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           const float x = KEEP ? rv(i, j) : (rv(i, j) - off2[j]) * r2[j], g = KEEP ? dv(i, j) : dv(i, j) * p2[j];
-          const float y = (av(i, j) - off1[j]) * (mine ? r1[j] : 0.0f);
+          const float y = (av(i, j) - off1[j]) * r1[j];
           o[j] = fmaf(r2[j], g - fmaf(x, m2[j], mz[j]), a.dr ? qv(i, j) : 0.0f);
           const float d = there(i, j) ? o[j] : 0.0f;
           uo[j] = there(i, j) ? d * open[j] : 0.0f;
@@ -186,14 +188,14 @@ __global__ __launch_bounds__(MAXT) void k_res_backward(const ResArgs a, const Re
           v[j] = d * fmaf(p[j], y, b[j]);  // D s t
           if constexpr (K1) {
             v[j] *= open[j] * shut[j];
-            f0[i][j] = fmaf(uo[j], one, f0[i][j]);
+            f0[i][j] += uo[j];
           }
           g1[i][j] = u[j];
           av.set(i, j, y);
           q[j] = fmaf(u[j], y, q[j]);
           q0[j] += u[j];
         }
-        if constexpr (!K1) f0[i][0] = fmaf(pl.sum_zero(uo), one, f0[i][0]);
+        if constexpr (!K1) f0[i][0] += pl.sum_zero(uo);
         if (mine && a.dx) step_store<false, T, V>(static_cast<T*>(a.dx) + n * R, i * AV + V * t, R, o);
         if (a.dgate) {
           if constexpr (K1) {

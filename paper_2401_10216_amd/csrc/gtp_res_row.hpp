@@ -326,6 +326,10 @@ struct RowRegs {
   __device__ __forceinline__ void fix(int t, int AV, int R) {  // zeros past the end
     step_fix<false, T, V>(v[NI - 1], (NI - 1) * AV + V * t, R);
   }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) v[i] = typename Vec<T, V>::type{};
+  }
   __device__ __forceinline__ float operator()(int i, int j) const { return get<T, V>(v[i], j); }
   // fp32 rows only: something made of the element in its place
   __device__ __forceinline__ void set(int i, int j, float f) {
