@@ -657,7 +657,7 @@ def gtp_residual_norm_backward(r, a, L: int, stats, dh, dr=None, gate=None, scal
     """Gradients of <dh, h> + <dr, r> of gtp_residual_norm, whose results r and stats and other arguments it takes
     (dr None: zeros): a dict with the keys of need (None: all there are) among dx, da (like r), dgate[N, C] (with a
     gate), dscale[L+1, C], dw_post[L+1, C], db_post[C] (with post), dw_pre[L+1, C], db_pre[C] (fp32).  dx: a tensor to
-    write to, which may be dr."""
+    write to, which may be dr, if it is asked for."""
     import torch
     f32 = torch.float32
     desc, pr, pa = _residual(r, a, L, gate, scale, w_post, b_post, w_pre, b_pre, post, 1.0, "r")
@@ -668,6 +668,8 @@ def gtp_residual_norm_backward(r, a, L: int, stats, dh, dr=None, gate=None, scal
     unknown = set(need) - set(there)
     if unknown:
         raise ValueError(f"unknown gradients {sorted(unknown)}")
+    if dx is not None and "dx" not in need:
+        raise ValueError("dx is given, but not among need")
     if len(stats) != 4:
         raise ValueError("stats must be what gtp_residual_norm returned")
     ps = [_ptr_of(t, name, size, f32, dev, plain) if post or i > 1 else 0 for i, (t, name, size) in enumerate(zip(
@@ -688,7 +690,7 @@ def gtp_residual_norm_backward(r, a, L: int, stats, dh, dr=None, gate=None, scal
             else:
                 out[n] = torch.empty((C,) if n.startswith("db") else (L + 1, C), dtype=f32, device=dev)
         work = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes > 0 else None
-    if dx is not None and "dx" in out:
+    if dx is not None:
         _ptr_of(dx, "dx", shape, own, dev, plain)
     _check(lib_.gtp_residual_norm_backward(d, pr, pa, _RESIDUAL_STATS.pack(*ps), pdh, pdr,
                                            _RESIDUAL_GRADS.pack(*[_ptr(out.get(n)) or 0 for n in _RESIDUAL_NEED]),
@@ -901,13 +903,15 @@ def gtp_attention_biased_backward(q, k, v, bias, q_pos, k_pos, r0, per_octave, o
                                   need=("dq", "dk", "dv", "dbias"), dq=None, dk=None, dv=None, stream=None):
     """Gradients of <do, gtp_attention_biased(q, k, v, bias, ...)[0]>: a dict with the requested keys among dq, dk, dv
     (dk and dv go together) and dbias[H, buckets] (fp32).  Arguments as the forward had them, o, lse as it returned
-    them; dq, dk, dv: tensors to write to."""
+    them; dq, dk, dv: tensors to write to, for what is asked for."""
     import torch
     desc, rows = _attn(q, k, v, scale, q_off, k_off, max_q, max_k, key_mask, p, rng)
     b = _bias(bias, q_pos, k_pos, r0, per_octave, q, k)
     need = set(need)
     if need - {"dq", "dk", "dv", "dbias"}:
         raise ValueError(f"unknown gradients {sorted(need - {'dq', 'dk', 'dv', 'dbias'})}")
+    if (dq is not None and "dq" not in need) or ((dk is not None or dv is not None) and not need & {"dk", "dv"}):
+        raise ValueError("dq, dk or dv is given, but not among need")
     dev, dt, qs, ks = q.device, q.dtype, q.shape, k.shape
     ro = _attn_rows(o, "o", qs, dt, dev)
     rdo = _attn_rows(do, "do", qs, dt, dev)

@@ -63,3 +63,20 @@ def test_rows_on_both_sides_of_the_limit(n, dtype):
     assert bool(((total(grads["dv"]) - total(do)).abs() <= (c + 2 * half) * size).all())
     rows = (do.double().abs().sum(-1) * v.double().abs().amax((0, 2))).sum(0) * 2  # of |dS| by head
     assert bool((grads["dbias"].double().sum(1).abs() <= c * rows + half * (do.double() * o.double()).abs().sum((0, 2))).all())
+
+
+def test_outputs_that_are_not_asked_for():
+    """Refused before anything else happens: they would stay as they were."""
+    z = torch.zeros
+    q, k, lse, pos = z(6, 4, 8), z(6, 2, 8), z(6, 4), z(6, 3)
+
+    def call(need, **out):
+        gtp.gtp_attention_biased_backward(q, k, k, z(4, 16), pos, None, 1.0, 4, q, q, lse, need=need, **out)
+
+    for need, name in ((("dk", "dv"), "dq"), (("dbias",), "dq"), (("dq",), "dk"), (("dq", "dbias"), "dv"), ((), "dq")):
+        with pytest.raises(ValueError, match="not among need"):
+            call(need, **{name: torch.zeros_like(q if name == "dq" else k)})
+    # dk and dv are made together: either may be given where one is asked for
+    for need, name in ((("dq",), "dq"), (("dk",), "dv"), (("dv",), "dk")):
+        with pytest.raises(ValueError, match="device tensor"):
+            call(need, **{name: torch.zeros_like(q if name == "dq" else k)})

@@ -1,4 +1,5 @@
-"""Limits of the residual step: infinities in the gradients of the last rows (-m gpu)."""
+"""Limits of the residual step: outputs that are not asked for (on the CPU); infinities in the gradients of the last rows
+(-m gpu)."""
 import math
 
 import pytest
@@ -42,3 +43,15 @@ def test_infinities_of_the_last_row_stay_in_their_sums(N, C, L, dtype):
         t = xh[n] * c.w["w_post"][0, 1].double(), c.w["b_post"][1].double()
         if float(t[0]) * float(t[1]) > 0:
             assert float(g["dscale"][0, 1]) == math.copysign(math.inf, -float(t[0]))
+
+
+def test_dx_that_is_not_asked_for():
+    """Refused before anything else happens: it would stay as it was."""
+    z = torch.zeros
+    x, st = z(4, 8, 9), (z(4), z(4, 3), z(4), z(4, 3))
+    for need in (("da",), ("dscale", "dw_pre"), ()):
+        with pytest.raises(ValueError, match="dx is given"):
+            gtp.gtp_residual_norm_backward(x, x, 2, st, x, need=need, dx=z(4, 8, 9))
+    for need in (None, ("dx", "da")):  # asked for: the next refusal, of tensors in host memory
+        with pytest.raises(ValueError, match="device tensor"):
+            gtp.gtp_residual_norm_backward(x, x, 2, st, x, need=need, dx=z(4, 8, 9))
