@@ -848,10 +848,17 @@ def gtp_attention_backward(q, k, v, o, do, lse, scale=None, q_off=None, k_off=No
     return {n: t for n, t in out.items() if n in need}
 
 
+def _squared(r0):
+    """r0^2; a negative r0, whose square would do, is refused here, the rest by the library."""
+    if r0 < 0:
+        raise ValueError("r0 must be positive")
+    return r0 * r0
+
+
 def gtp_attention_bias_edges(buckets: int, r0: float, per_octave: int = 4) -> list:
     """The first squared distances of buckets 1 .. buckets - 1 of gtp_attention_biased."""
     out = (ctypes.c_float * max(buckets - 1, 1))()
-    _check(lib().gtp_attention_bias_edges(r0 * r0, buckets, per_octave, out))
+    _check(lib().gtp_attention_bias_edges(_squared(r0), buckets, per_octave, out))
     return list(out)[:buckets - 1]
 
 
@@ -866,7 +873,7 @@ def _bias(bias, q_pos, k_pos, r0, per_octave, q, k):
     pq = _ptr_of(q_pos, "q_pos", (Tq, 3), f32, dev, plain)
     pk = pq if k_pos is None and Tk == Tq else _ptr_of(k_pos, "k_pos", (Tk, 3), f32, dev, plain)
     try:
-        return _BIAS.pack(pb, pq, pk, r0 * r0, bias.shape[1], per_octave)
+        return _BIAS.pack(pb, pq, pk, _squared(r0), bias.shape[1], per_octave)
     except (OverflowError, struct.error) as e:  # beyond fp32, or not a whole number
         raise ValueError(f"r0 and per_octave must be a number and a whole number within range: {e}") from None
 

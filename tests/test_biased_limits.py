@@ -80,3 +80,16 @@ def test_outputs_that_are_not_asked_for():
     for need, name in ((("dq",), "dq"), (("dk",), "dv"), (("dv",), "dk")):
         with pytest.raises(ValueError, match="device tensor"):
             call(need, **{name: torch.zeros_like(q if name == "dq" else k)})
+
+
+def test_negative_r0():
+    """Its square would do for the library."""
+    z = torch.zeros
+    q, k, lse, pos, bias = z(6, 4, 8), z(6, 2, 8), z(6, 4), z(6, 3), z(4, 16)
+    for r0 in (-1.0, -1e-3, -1e30, -math.inf):
+        with pytest.raises(ValueError, match="r0"):
+            gtp.gtp_attention_biased(q, k, k, bias, pos, r0=r0)
+        with pytest.raises(ValueError, match="r0"):
+            gtp.gtp_attention_biased_backward(q, k, k, bias, pos, None, r0, 4, q, q, lse)
+        with pytest.raises(ValueError, match="r0"):
+            gtp.gtp_attention_bias_edges(16, r0)
