@@ -848,17 +848,22 @@ def gtp_attention_backward(q, k, v, o, do, lse, scale=None, q_off=None, k_off=No
     return {n: t for n, t in out.items() if n in need}
 
 
-def _squared(r0):
-    """r0^2; a negative r0, whose square would do, is refused here, the rest by the library."""
+def _bias_numbers(pointers, r0, buckets, per_octave):
+    """Packed gtp_attn_bias.  What its fields cannot hold, and a negative r0, whose square would do, are refused here, the
+    rest by the library."""
     if r0 < 0:
         raise ValueError("r0 must be positive")
-    return r0 * r0
+    try:
+        return _BIAS.pack(*pointers, r0 * r0, buckets, per_octave)
+    except (OverflowError, struct.error) as e:  # beyond fp32, or not a whole number of 32 bits
+        raise ValueError(f"r0, buckets and per_octave must be a number and whole numbers within range: {e}") from None
 
 
 def gtp_attention_bias_edges(buckets: int, r0: float, per_octave: int = 4) -> list:
     """The first squared distances of buckets 1 .. buckets - 1 of gtp_attention_biased."""
-    out = (ctypes.c_float * max(buckets - 1, 1))()
-    _check(lib().gtp_attention_bias_edges(_squared(r0), buckets, per_octave, out))
+    _bias_numbers((0, 0, 0), r0, buckets, per_octave)
+    out = (ctypes.c_float * 63)()  # of 64 buckets, the most there are
+    _check(lib().gtp_attention_bias_edges(r0 * r0, buckets, per_octave, out))
     return list(out)[:buckets - 1]
 
 
@@ -872,10 +877,7 @@ def _bias(bias, q_pos, k_pos, r0, per_octave, q, k):
     pb = _ptr_of(bias, "bias", (q.shape[1], bias.shape[1]), f32, dev, plain)
     pq = _ptr_of(q_pos, "q_pos", (Tq, 3), f32, dev, plain)
     pk = pq if k_pos is None and Tk == Tq else _ptr_of(k_pos, "k_pos", (Tk, 3), f32, dev, plain)
-    try:
-        return _BIAS.pack(pb, pq, pk, _squared(r0), bias.shape[1], per_octave)
-    except (OverflowError, struct.error) as e:  # beyond fp32, or not a whole number
-        raise ValueError(f"r0 and per_octave must be a number and a whole number within range: {e}") from None
+    return _bias_numbers((pb, pq, pk), r0, bias.shape[1], per_octave)
 
 
 def gtp_attention_biased(q, k, v, bias, q_pos, k_pos=None, r0: float = 1.0, per_octave: int = 4, scale=None, q_off=None,

@@ -93,3 +93,15 @@ def test_negative_r0():
             gtp.gtp_attention_biased_backward(q, k, k, bias, pos, None, r0, 4, q, q, lse)
         with pytest.raises(ValueError, match="r0"):
             gtp.gtp_attention_bias_edges(16, r0)
+
+
+def test_edges_of_numbers_out_of_range():
+    """Neither cut to 32 bits nor answered with a list of that many."""
+    for buckets, per in ((2 ** 32 + 4, 4), (4, 2 ** 32 + 4), (-(2 ** 32) + 4, 4), (2 ** 70, 4), (4, 4.0), (4.0, 4), (10 ** 9, 4), (65, 4),
+                         (-1, 4), (0, 4)):
+        with pytest.raises((ValueError, gtp.GTPError)):
+            gtp.gtp_attention_bias_edges(buckets, 1.0, per)
+    with pytest.raises((ValueError, gtp.GTPError)):
+        gtp.gtp_attention_bias_edges(4, 1e200)
+    assert gtp.gtp_attention_bias_edges(4, 1.0, 1) == [1.0, 2.0, 4.0] and gtp.gtp_attention_bias_edges(1, 1.0) == []
+    assert len(gtp.gtp_attention_bias_edges(64, 1.0)) == 63
