@@ -664,7 +664,7 @@ def gtp_residual_norm_backward(r, a, L: int, stats, dh, dr=None, gate=None, scal
     N, C, _ = shape = r.shape
     dev, own, plain = r.device, r.dtype, torch.Tensor
     there = [n for n in _RESIDUAL_NEED if (gate is not None or n != "dgate") and (post or not n.endswith("_post"))]
-    need = there if need is None else need
+    need = there if need is None else tuple(need)
     unknown = set(need) - set(there)
     if unknown:
         raise ValueError(f"unknown gradients {sorted(unknown)}")

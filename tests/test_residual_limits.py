@@ -55,3 +55,14 @@ def test_dx_that_is_not_asked_for():
     for need in (None, ("dx", "da")):  # asked for: the next refusal, of tensors in host memory
         with pytest.raises(ValueError, match="device tensor"):
             gtp.gtp_residual_norm_backward(x, x, 2, st, x, need=need, dx=z(4, 8, 9))
+
+
+@pytest.mark.gpu
+def test_need_may_be_any_iterable():
+    c = Case(5, 16, 2, 1, F32, device="cuda")
+    r, _, stats = c.forward()
+    all_ = c.backward(r, stats)
+    for names in (("dx", "dscale"), ("da",), ("dgate", "db_pre"), ("dw_post", "dw_post"), ()):
+        for need in (names, iter(names), set(names), (n for n in names)):
+            got = c.backward(r, stats, need=need)
+            assert set(got) == set(names) and all(torch.equal(got[n], all_[n]) for n in names)
