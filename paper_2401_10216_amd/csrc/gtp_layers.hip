@@ -474,6 +474,10 @@ gtp_status bias_args(const gtp_attn_bias* b, gtp::AttnArgs* g) {
   return GTP_OK;
 }
 
+gtp_status work_too_small(bool biased) {
+  return bad(biased ? "work is smaller than gtp_attention_biased_work says" : "work is smaller than gtp_attention_work says");
+}
+
 // Checks of `n` inputs and outputs against each other, the row statistics, the
 // work and the index arrays.
 gtp_status attn_memory(const gtp_attn* a, const Rows* in, int n_in, const Rows* out, int n_out, Span lse, bool lse_out,
@@ -529,7 +533,7 @@ gtp_status attention(const gtp_attn* a, const gtp_attn_bias* b, bool biased, con
   if (s == GTP_OK && biased) s = bias_args(b, &g);
   if (s != GTP_OK) return s;
   const int64_t need = attn_work(g, 0);
-  if (need > 0 && (!work || work_bytes < need)) return bad("work is smaller than its size function says");
+  if (need > 0 && (!work || work_bytes < need)) return work_too_small(biased);
   if (a->Tq > 0 && !o) return bad("NULL data pointer");
   const Rows in[] = {{q, a->Tq, a->H}, {k, a->Tk, a->Hk}, {v, a->Tk, a->Hk}}, out[] = {{o, a->Tq, a->H}};
   s = attn_memory(a, in, 3, out, 1, {lse, a->Tq * a->H * 4}, true, {need > 0 ? work : nullptr, need}, &g.vec, b, {});
@@ -564,7 +568,7 @@ gtp_status attention_backward(const gtp_attn* a, const gtp_attn_bias* b, bool bi
   if (!dq && !dk && !dbias) return GTP_OK;
   if (!aligned(dbias, 4)) return bad("misaligned pointer");
   const int64_t need = attn_work(g, 1);
-  if (need > 0 && (!work || work_bytes < need)) return bad("work is smaller than its size function says");
+  if (need > 0 && (!work || work_bytes < need)) return work_too_small(biased);
   const Rows in[] = {{q, a->Tq, a->H}, {k, a->Tk, a->Hk}, {v, a->Tk, a->Hk}, {o, a->Tq, a->H}, {dout, a->Tq, a->H}};
   const Rows out[] = {{dq, a->Tq, a->H}, {dk, a->Tk, a->Hk}, {dv, a->Tk, a->Hk}};
   s = attn_memory(a, in, 5, out, 3, {lse, a->Tq * a->H * 4}, false, {need > 0 ? work : nullptr, need}, &g.vec, b,

@@ -10,7 +10,7 @@ torch = pytest.importorskip("torch")
 import biased_ref as B  # noqa: E402
 from paper_2401_10216_amd import gtp  # noqa: E402
 from test_biased_host import bias_desc  # noqa: E402
-from test_layers_host import attn_desc  # noqa: E402
+from test_layers_host import at, attn_desc, rows  # noqa: E402
 
 
 def test_work_stays_bounded_for_large_segments():
@@ -105,3 +105,16 @@ def test_edges_of_numbers_out_of_range():
         gtp.gtp_attention_bias_edges(4, 1e200)
     assert gtp.gtp_attention_bias_edges(4, 1.0, 1) == [1.0, 2.0, 4.0] and gtp.gtp_attention_bias_edges(1, 1.0) == []
     assert len(gtp.gtp_attention_bias_edges(64, 1.0)) == 63
+
+
+def test_too_little_work_names_its_size_function():
+    lib, a = gtp.lib(), attn_desc(Tk=20000, max_k=20000)
+    r = [ctypes.byref(rows(i, h)) for i, h in ((0, 4), (1, 2), (2, 2), (3, 4))]
+    back = [ctypes.byref(rows(i, h)) for i, h in ((4, 4), (7, 4), (8, 2), (9, 2))]
+    for name, biased in (("gtp_attention", ()), ("gtp_attention_biased", (bias_desc(),))):
+        assert getattr(lib, name)(ctypes.byref(a), *biased, *r, at(5), at(6), 16, None) == gtp.GTP_ERR_INVALID_ARG
+        assert name + "_work" in lib.gtp_last_error().decode()
+        more = (at(43),) if biased else ()
+        assert getattr(lib, name + "_backward")(ctypes.byref(a), *biased, *r, back[0], at(5), *back[1:], *more, at(6), 16,
+                                                None) == gtp.GTP_ERR_INVALID_ARG
+        assert name + "_work" in lib.gtp_last_error().decode()
