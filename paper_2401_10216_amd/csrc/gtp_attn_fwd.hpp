@@ -32,6 +32,9 @@
 // With a bias by distance (see Buckets) a score takes twice the vector instructions, 20 instead of 10, or, with its
 // bucket made ahead for all heads (gtp_attn_bytes.hip), 11 and an LDS read.  8192 rows, 8 heads of 128, 32 buckets,
 // bf16: 549 us so, 447 with the buckets made ahead (their making 20 of it).  Molecules as above: 25.3 us.
+// fp32, 8192 rows, 8 heads of 128: 1715 us (without a bias 1590), two of 1777-2001 rows, 8 heads of 64: 140 (122).  Few rows: 4
+// against 15000-16001 keys, 8 heads over 2 of 64: bf16 28 us (22), fp32 66 (57); one against 60000, 8 heads of 128: bf16 123 (65),
+// fp32 442 (381): workgroups of 64 rows, whose buckets and bias spill there (196 and 376 bytes a lane).
 #pragma once
 
 #include "gtp_attn_core.hpp"

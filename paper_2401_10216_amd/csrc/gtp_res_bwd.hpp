@@ -278,7 +278,7 @@ __global__ __launch_bounds__(MAXT) void k_res_backward(const ResArgs a, const Re
 
 // Workgroups: as many as the CUs hold at once (each makes the tables and leaves a part of the weights' gradients), and
 // two rows a team at least, where that fills the chip.  50001 rows of 500 scalars, bf16, 2 steps of a wave: 512 workgroups
-// 100 us, 768 86, 1024 110.
+// 100 us, 768 86, 1024 110 (three fit a CU: 146 registers a lane, and 49 KB of LDS each with the room for gates that scalars leave unused).
 inline int64_t res_grid(int64_t N, const ResLay& y) {
   const int64_t rows = (N + y.teams() - 1) / y.teams();
   const int64_t n = std::min<int64_t>(rows, y.threads > kTeamThreads || y.NI > 4 ? 256 : y.NI > 2 ? 512 : 768),

@@ -152,7 +152,9 @@ bool wide16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 constexpr int64_t kMaxLds = 150 << 10;
 
-// LDS bytes of a layout; back: the gradient's, which has the teams' elements besides.
+// LDS bytes of a layout; back: the gradient's, which has the teams' elements besides.  The gates' room is counted for every
+// row, also for scalars, whose gates lie in registers: that, not the registers, ends their layouts at 7168 scalars, gradient
+// 4096.
 int64_t res_lds(const ResLay& y, int64_t K, int L, bool back) {
   const int64_t AV = int64_t(y.A) * y.V, elements = y.NI * AV, channels = elements / K;
   const int64_t block = y.W ? 0 : (K == 1 ? 2 * int64_t(y.A) : AV + AV / K) + L + 2;
@@ -183,7 +185,9 @@ bool residual_layout(const ResArgs& a, bool wide, bool back, ResLay* out) {
     const ResLay y{0, V, int(steps), int(A), int(threads)};
     // the share of lanes and steps at work, less where a workgroup's registers leave the CU no second one (of 256
     // threads; of 512, no second wave on a SIMD): 6272 elements, fp32, backward: 355 us on 512 threads in 4 steps, 450 on 256
-    // in 7; bf16, forward: 383 on 512 in 2 steps of 8, 473 on 256 in 4
+    // in 7; bf16, forward: 383 on 512 in 2 steps of 8, 473 on 256 in 4.  Even 512 threads in 5 to 8 steps, which spill, are ahead
+    // of a row that is read for each pass: 4000 x 9720 elements, fp32, backward 384 us in 5 (1193), 10368 in 6 513 (1450), bf16
+    // 269 and 391 (1022 and 1304)
     const int64_t few = back ? (threads > kTeamThreads ? 4 : 3) : (threads > kTeamThreads ? 16 : 20) / V;
     const double use = double(R) / (double(threads) * V * double(steps)) *
                        (threads > kTeamThreads ? 0.95 : 1.0) * (steps <= few ? 1.0 : back && threads > kTeamThreads ? 0.5 : 0.75);

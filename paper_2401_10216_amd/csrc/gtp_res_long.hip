@@ -7,7 +7,8 @@
 // gradient; the weights' sums, by workgroups that walk down the rows in the places of one step; the rows'
 // gradients: five reads of a tensor forward where rows in registers take two, fourteen backward for four, and weights
 // gathered by channel.  1200 x 512 channels of degree 8, fp32: 593 us forward and 1330 backward (1.3 and 0.9 TB/s of what has
-// to move; a degree at a time, gtp_res_any.hip: 1140 and 5520).
+// to move; a degree at a time, gtp_res_any.hip: 1146 and 2922); bf16: 580 and 1205 (1008 and 2689), so that it is not the
+// bytes that bound it but the gathers, four addresses a thread and table in every pass.
 #include <algorithm>
 
 #include "gtp_res_row.hpp"
